@@ -457,6 +457,107 @@ higgs_status higgs_qmatmul_fused_multi(int layers, const void *x, higgs_dtype x_
                                        const int64_t *out, int64_t in, float *const *y,
                                        void *workspace, int64_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Microscaled layers: 4-bit floats with one power of two per 32 weights, the
+ * format that gfx950's matrix cores multiply without a lookup table, with the
+ * rotation of App. G or without one; an option of 4.25 bits per weight beside
+ * the grids of Alg. 2 (Sec. 4 chooses per layer by t^2 and bits).
+ *
+ * A row is cut into blocks of 32 consecutive values (the last one padded with
+ * zeros where in % 32 != 0); blocks = ceil(in / 32). Per block:
+ *   E     = max(floor(log2 a) - 2, -127), a the largest magnitude of the block
+ *           (E = -127 where a = 0); scale byte E + 127.
+ *   codes = the values v 2^-E rounded to the format, to nearest with ties to
+ *           even, magnitudes above its largest to that. The sign is kept, also
+ *           of zeros. A code stands for c 2^E, c its format's value.
+ * Formats (sign, two exponent bits of bias 1, mantissa):
+ *   HIGGS_MX_FP4  E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6. 16 bytes per block: code j
+ *                 in bits [4j, 4j + 4), least significant first.
+ *   HIGGS_MX_FP6  E2M3: multiples of 1/8 to 2, of 1/4 to 4, of 1/2 to 7.5. 24
+ *                 bytes per block: code j in bits [6j, 6j + 6).
+ * A block that holds a NaN, an infinity or, after the rotation, a magnitude of
+ * 2^128 or more has scale byte 255 and codes 0; all its values are NaN, and
+ * every output that sums over it.
+ * codes: uint8 [rows][blocks * 16 or 24]; scales: uint8 [rows][blocks].
+ * g: 0 for no rotation, or a power of two in [64, 4096] with in % g == 0: the
+ * rows are rotated in groups of g as for higgs_quantize, with rht_seed, before
+ * they are cut into blocks. The rotation is computed in fp64; zeros that it
+ * gives are positive.
+ * ------------------------------------------------------------------------- */
+typedef enum higgs_mx_format {
+  HIGGS_MX_FP4 = 0,
+  HIGGS_MX_FP6 = 1,
+  /* Range markers, as for higgs_dtype. */
+  HIGGS_MX_FORMAT_RANGE_MIN_ = -2147483647 - 1,
+  HIGGS_MX_FORMAT_RANGE_MAX_ = 2147483647
+} higgs_mx_format;
+
+/* Bytes of one row of codes (blocks * 16 or 24) and of scales (blocks); -1 if
+ * the arguments are invalid. Host only, pure. */
+int64_t higgs_mx_codes_row_bytes(int64_t in, higgs_mx_format fmt);
+int64_t higgs_mx_scales_row_bytes(int64_t in);
+
+/* higgs_mx_quantize - W [rows][in] (weights, or activations) to codes and
+ * scales. Device, asynchronous on `stream`, one launch.
+ *   W       [in]  device, rows*in values of w_dtype, 16-byte aligned.
+ *   codes   [out] device, rows * higgs_mx_codes_row_bytes(in, fmt) bytes,
+ *                 16-byte aligned.
+ *   scales  [out] device, rows * higgs_mx_scales_row_bytes(in) bytes.
+ * Requires rows >= 1, in >= 1, rows * in < 2^40. */
+higgs_status higgs_mx_quantize(const void *W, higgs_dtype w_dtype, int64_t rows, int64_t in,
+                               higgs_mx_format fmt, int g, uint64_t rht_seed, uint8_t *codes,
+                               uint8_t *scales, void *stream);
+
+/* higgs_mx_dequantize - codes and scales to W [rows][in] of w_dtype. With
+ * g = 0 the stored values (of rotated rows: in the rotated space); with the g
+ * and rht_seed of the quantization the values rotated back,
+ * sigma * H(values) / sqrt(g) per group. Device, asynchronous, one launch.
+ *   codes   [in]  device, 16-byte aligned; any codes and scale bytes.
+ *   W       [out] device, rows*in values, 16-byte aligned.
+ * Requirements as for higgs_mx_quantize. */
+higgs_status higgs_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows,
+                                 int64_t in, higgs_mx_format fmt, int g, uint64_t rht_seed,
+                                 void *W, higgs_dtype w_dtype, void *stream);
+
+/* higgs_mx_layer_error - the error of a HIGGS_MX_FP4 layer (Sec. 3.4), for
+ * higgs_allocate_bits as higgs_layer_error for the grids. Device, asynchronous.
+ *   row_err  [out] device, 2*out doubles, 8-byte aligned: per row o
+ *            ||W[o] - W_hat[o]||^2 (in the rotated space where g > 0, where it is
+ *            the same) and ||W[o]||^2, fp64, summed in a fixed order.
+ *   t2       [out] device, nullable, one double: the ratio of their totals (0
+ *            for an all-zero layer).
+ * Other arguments as for higgs_mx_quantize. W must hold finite values (others
+ * make the row's error and t2 NaN or infinite). Requires out < 2^31. */
+higgs_status higgs_mx_layer_error(const void *W, higgs_dtype w_dtype, int64_t out, int64_t in,
+                                  const uint8_t *codes, const uint8_t *scales, int g,
+                                  uint64_t rht_seed, double *row_err, double *t2, void *stream);
+
+/* higgs_mx_qmatmul - the output of a HIGGS_MX_FP4 layer from raw activations:
+ *   y = x_hat W_hat^T,
+ * x_hat the activations as higgs_mx_quantize(x, x_fmt, g, rht_seed) stores them
+ * (HIGGS_MX_FP4, or HIGGS_MX_FP6 with about a quarter of its error), W_hat the
+ * layer's stored values. The conversion is part of the call. Products are exact,
+ * sums fp32; y is fp32 or bf16 (rounded once). Device, asynchronous.
+ *   x          [in]  device, batch*in values of x_dtype, 16-byte aligned.
+ *   codes      [in]  device, out * blocks * 16 bytes, 16-byte aligned.
+ *   scales     [in]  device, out * blocks bytes.
+ *   g, rht_seed  those of the layer's higgs_mx_quantize.
+ *   y          [out] device, batch*out values of y_dtype, 16-byte aligned. Must
+ *                    not overlap the inputs or the workspace.
+ *   workspace  [in]  device scratch of at least
+ *                    higgs_mx_qmatmul_workspace_bytes(...) bytes, 256-byte
+ *                    aligned (may be NULL when that is 0); not preserved. Calls
+ *                    that overlap in time need workspaces of their own.
+ * Requires batch >= 1, out >= 1, in >= 1, batch * in < 2^40, in <= 2^20,
+ * codes below 2 GiB (HIGGS_ERR_UNSUPPORTED otherwise). */
+int64_t higgs_mx_qmatmul_workspace_bytes(int64_t batch, int64_t out, int64_t in,
+                                         higgs_mx_format x_fmt, int g);
+higgs_status higgs_mx_qmatmul(const void *x, higgs_dtype x_dtype, int64_t batch,
+                              higgs_mx_format x_fmt, const uint8_t *codes, const uint8_t *scales,
+                              int g, uint64_t rht_seed, int64_t out, int64_t in, void *y,
+                              higgs_dtype y_dtype, void *workspace, int64_t workspace_bytes,
+                              void *stream);
+
 #ifdef __cplusplus
 }
 #endif

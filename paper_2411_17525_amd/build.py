@@ -32,6 +32,8 @@ SOURCES = {
     "qgemm.hip": [],
     "qgemm_wide.hip": [],
     "scratch.hip": [],
+    "mx_quant.hip": [],
+    "mx_product.hip": [],
 }
 
 

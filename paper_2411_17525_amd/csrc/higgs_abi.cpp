@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "internal.h"
+#include "mx.h"
 
 namespace {
 
@@ -509,6 +510,141 @@ higgs_status higgs_qmatmul_fused_multi(int layers, const void* x, higgs_dtype x_
     if (st != HIGGS_OK) return st;
   }
   return ok();
+}
+
+}  // extern "C"
+
+// ---- microscaled layers ----
+
+namespace {
+
+// Shared checks of the microscaled entry points.
+higgs_status check_mx(higgs_dtype dtype, const char* dtype_name, int64_t rows, int64_t in, int fmt,
+                      int g) {
+  if (dtype != HIGGS_F32 && dtype != HIGGS_BF16)
+    return fail(HIGGS_ERR_INVALID_ARG, "%s must be HIGGS_F32 or HIGGS_BF16", dtype_name);
+  if (fmt != HIGGS_MX_FP4 && fmt != HIGGS_MX_FP6)
+    return fail(HIGGS_ERR_INVALID_ARG, "the format must be HIGGS_MX_FP4 or HIGGS_MX_FP6");
+  if (rows < 1 || in < 1)
+    return fail(HIGGS_ERR_INVALID_ARG, "rows (%lld) and in (%lld) must be >= 1", (long long)rows,
+                (long long)in);
+  if (g != 0) {
+    if (higgs::log2_exact(g) < 0)
+      return fail(HIGGS_ERR_INVALID_ARG, "g (%d) must be 0 or a power of two", g);
+    if (g < 64 || g > 4096)
+      return fail(HIGGS_ERR_UNSUPPORTED, "g=%d not supported: need 64 <= g <= 4096, or 0", g);
+    if (in % g != 0)
+      return fail(HIGGS_ERR_INVALID_ARG, "in (%lld) must be a multiple of g (%d)", (long long)in,
+                  g);
+  }
+  if (rows > (int64_t(1) << 40) / in)
+    return fail(HIGGS_ERR_UNSUPPORTED, "rows * in must be below 2^40");
+  return HIGGS_OK;
+}
+
+higgs_status check_mx_product(int64_t batch, int64_t out, int64_t in, int fmt, int g) {
+  higgs_status st = check_mx(HIGGS_F32, "", batch, in, fmt, g);
+  if (st == HIGGS_OK) st = check_mx(HIGGS_F32, "", out, in, fmt, g);
+  if (st != HIGGS_OK) return st;
+  if (in > (int64_t(1) << 20))
+    return fail(HIGGS_ERR_UNSUPPORTED, "in (%lld) above 2^20 is not supported", (long long)in);
+  // the kernels address codes with 32-bit byte offsets
+  if (out * higgs::mx_blocks(in) * 16 >= (int64_t(1) << 31))
+    return fail(HIGGS_ERR_UNSUPPORTED, "layer too large: codes must be < 2 GiB");
+  if (batch > (int64_t(1) << 40) / out)
+    return fail(HIGGS_ERR_UNSUPPORTED, "batch * out must be below 2^40");
+  return HIGGS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t higgs_mx_codes_row_bytes(int64_t in, higgs_mx_format fmt) {
+  if (in < 1 || in > (int64_t(1) << 40) || (fmt != HIGGS_MX_FP4 && fmt != HIGGS_MX_FP6)) return -1;
+  return higgs::mx_blocks(in) * higgs::mx_block_bytes(fmt);
+}
+
+int64_t higgs_mx_scales_row_bytes(int64_t in) {
+  if (in < 1 || in > (int64_t(1) << 40)) return -1;
+  return higgs::mx_blocks(in);
+}
+
+higgs_status higgs_mx_quantize(const void* W, higgs_dtype w_dtype, int64_t rows, int64_t in,
+                               higgs_mx_format fmt, int g, uint64_t rht_seed, uint8_t* codes,
+                               uint8_t* scales, void* stream) {
+  if (!W || !codes || !scales)
+    return fail(HIGGS_ERR_INVALID_ARG, "W, codes and scales must not be NULL");
+  const higgs_status st = check_mx(w_dtype, "w_dtype", rows, in, fmt, g);
+  if (st != HIGGS_OK) return st;
+  if (!aligned(W, 16) || !aligned(codes, 16))
+    return fail(HIGGS_ERR_INVALID_ARG, "W and codes must be 16-byte aligned");
+  return device_status(higgs::launch_mx_quantize(W, w_dtype, rows, in, fmt, g, rht_seed, codes,
+                                                 scales, static_cast<hipStream_t>(stream)),
+                       "higgs_mx_quantize launch");
+}
+
+higgs_status higgs_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows,
+                                 int64_t in, higgs_mx_format fmt, int g, uint64_t rht_seed,
+                                 void* W, higgs_dtype w_dtype, void* stream) {
+  if (!W || !codes || !scales)
+    return fail(HIGGS_ERR_INVALID_ARG, "codes, scales and W must not be NULL");
+  const higgs_status st = check_mx(w_dtype, "w_dtype", rows, in, fmt, g);
+  if (st != HIGGS_OK) return st;
+  if (!aligned(W, 16) || !aligned(codes, 16))
+    return fail(HIGGS_ERR_INVALID_ARG, "W and codes must be 16-byte aligned");
+  return device_status(higgs::launch_mx_dequantize(codes, scales, rows, in, fmt, g, rht_seed, W,
+                                                   w_dtype, static_cast<hipStream_t>(stream)),
+                       "higgs_mx_dequantize launch");
+}
+
+higgs_status higgs_mx_layer_error(const void* W, higgs_dtype w_dtype, int64_t out, int64_t in,
+                                  const uint8_t* codes, const uint8_t* scales, int g,
+                                  uint64_t rht_seed, double* row_err, double* t2, void* stream) {
+  if (!W || !codes || !scales || !row_err)
+    return fail(HIGGS_ERR_INVALID_ARG, "W, codes, scales and row_err must not be NULL");
+  const higgs_status st = check_mx(w_dtype, "w_dtype", out, in, HIGGS_MX_FP4, g);
+  if (st != HIGGS_OK) return st;
+  if (out >= (int64_t(1) << 31))
+    return fail(HIGGS_ERR_UNSUPPORTED, "out (%lld) must be below 2^31", (long long)out);
+  if (!aligned(W, 16) || !aligned(codes, 16) || !aligned(row_err, 8) || !aligned(t2, 8))
+    return fail(HIGGS_ERR_INVALID_ARG,
+                "W and codes must be 16-byte aligned, row_err and t2 8");
+  return device_status(higgs::launch_mx_layer_error(W, w_dtype, out, in, codes, scales, g,
+                                                    rht_seed, row_err, t2,
+                                                    static_cast<hipStream_t>(stream)),
+                       "higgs_mx_layer_error launch");
+}
+
+int64_t higgs_mx_qmatmul_workspace_bytes(int64_t batch, int64_t out, int64_t in,
+                                         higgs_mx_format x_fmt, int g) {
+  if (check_mx_product(batch, out, in, x_fmt, g) != HIGGS_OK) return -1;
+  return higgs::mx_qmatmul_workspace_bytes(batch, out, in, x_fmt, g);
+}
+
+higgs_status higgs_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch,
+                              higgs_mx_format x_fmt, const uint8_t* codes, const uint8_t* scales,
+                              int g, uint64_t rht_seed, int64_t out, int64_t in, void* y,
+                              higgs_dtype y_dtype, void* workspace, int64_t workspace_bytes,
+                              void* stream) {
+  if (!x || !codes || !scales || !y)
+    return fail(HIGGS_ERR_INVALID_ARG, "x, codes, scales and y must not be NULL");
+  if (x_dtype != HIGGS_F32 && x_dtype != HIGGS_BF16)
+    return fail(HIGGS_ERR_INVALID_ARG, "x_dtype must be HIGGS_F32 or HIGGS_BF16");
+  if (y_dtype != HIGGS_F32 && y_dtype != HIGGS_BF16)
+    return fail(HIGGS_ERR_INVALID_ARG, "y_dtype must be HIGGS_F32 or HIGGS_BF16");
+  const higgs_status st = check_mx_product(batch, out, in, x_fmt, g);
+  if (st != HIGGS_OK) return st;
+  const int64_t need = higgs::mx_qmatmul_workspace_bytes(batch, out, in, x_fmt, g);
+  if (workspace_bytes < need || (need > 0 && workspace == nullptr))
+    return fail(HIGGS_ERR_INVALID_ARG, "workspace too small: %lld bytes needed", (long long)need);
+  if (!aligned(x, 16) || !aligned(codes, 16) || !aligned(y, 16) || !aligned(workspace, 256))
+    return fail(HIGGS_ERR_INVALID_ARG,
+                "x, codes and y must be 16-byte aligned, workspace 256");
+  return device_status(higgs::launch_mx_qmatmul(x, x_dtype, batch, x_fmt, codes, scales, g,
+                                                rht_seed, out, in, y, y_dtype, workspace,
+                                                static_cast<hipStream_t>(stream)),
+                       "higgs_mx_qmatmul launch");
 }
 
 }  // extern "C"

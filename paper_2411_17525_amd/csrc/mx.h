@@ -1,0 +1,128 @@
+// The microscaled (MX) formats: blocks of 32 consecutive values of a row, each
+// value a 4-bit (E2M1) or 6-bit (E2M3) float, with one power of two per block
+// (E8M0: the byte is the exponent + 127). Shared by mx_quant.hip and
+// mx_product.hip.
+#pragma once
+
+#include "internal.h"
+
+namespace higgs {
+
+constexpr int kMxBlock = 32;
+// Both element formats have a largest binary exponent of 2 (6 and 7.5), so a
+// block's exponent is that of its largest magnitude less 2.
+constexpr int kMxTop = 2;
+
+inline int mx_block_bytes(int fmt) { return fmt == HIGGS_MX_FP4 ? 16 : 24; }
+inline int64_t mx_blocks(int64_t in) { return (in + kMxBlock - 1) / kMxBlock; }
+
+// RHT signs of a group of up to 4096: bit j % 32 of word j / 32 set iff
+// sigma_j = -1. A kernel argument: the kernels read it like any other.
+struct MxSigns {
+  uint32_t w[128];
+};
+// (mx_quant.hip; computed once per seed and group size, kept per thread)
+void mx_signs(uint64_t seed, int g, MxSigns* s);
+
+// Kernel launchers. g = 0: no rotation. The arguments have been checked.
+hipError_t launch_mx_quantize(const void* w, higgs_dtype dtype, int64_t rows, int64_t in, int fmt,
+                              int g, uint64_t seed, uint8_t* codes, uint8_t* scales,
+                              hipStream_t stream);
+hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows,
+                                int64_t in, int fmt, int g, uint64_t seed, void* w,
+                                higgs_dtype dtype, hipStream_t stream);
+hipError_t launch_mx_layer_error(const void* w, higgs_dtype dtype, int64_t out, int64_t in,
+                                 const uint8_t* codes, const uint8_t* scales, int g, uint64_t seed,
+                                 double* row_err, double* t2, hipStream_t stream);
+int64_t mx_qmatmul_workspace_bytes(int64_t batch, int64_t out, int64_t in, int fmt, int g);
+hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, int fmt,
+                             const uint8_t* codes, const uint8_t* scales, int g, uint64_t seed,
+                             int64_t out, int64_t in, void* y, higgs_dtype y_dtype,
+                             void* workspace, hipStream_t stream);
+
+// ---- device: one value ----
+
+// 2^e for e in [-126, 127] as fp32, or the E8M0 byte's power of two (0 is
+// 2^-127, a subnormal; 255 is NaN).
+__device__ inline float mx_scale_value(uint32_t byte) {
+  if (byte == 255) return __builtin_bit_cast(float, 0x7fc00000u);
+  return __builtin_bit_cast(float, byte == 0 ? 0x00400000u : byte << 23);
+}
+
+// A double rounded to 21 significant bits towards zero with the last bit set
+// where anything was dropped (round to odd), as fp32: rounding that again to
+// nearest, ties to even, to any format of up to 19 bits gives what one rounding
+// of the double gives. Exact in fp32 where |v| is 0 or in its normal range.
+__device__ inline float mx_odd_f32(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = uint32_t(u), hi = uint32_t(u >> 32);
+  return float(__builtin_bit_cast(double, uint64_t(hi | (lo < 1u ? lo : 1u)) << 32));
+}
+
+// 16 scaled values (|v| < 8) to codes, rounded to nearest with ties to even and
+// saturated: 2 words of E2M1 codes, or 3 of E2M3, the least significant bits
+// first.
+template <int FMT>
+__device__ inline void mx_encode16(const float (&v)[16], uint32_t* out) {
+  if constexpr (FMT == HIGGS_MX_FP4) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t r = 0;
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[8 * h], v[8 * h + 1], 1.0f, 0);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[8 * h + 2], v[8 * h + 3], 1.0f, 1);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[8 * h + 4], v[8 * h + 5], 1.0f, 2);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[8 * h + 6], v[8 * h + 7], 1.0f, 3);
+      out[h] = r;
+    }
+  } else {
+    // the instruction takes the even and the odd values of 32
+    typedef float f32x16 __attribute__((ext_vector_type(16)));
+    f32x16 even = {}, odd = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      even[i] = v[2 * i];
+      odd[i] = v[2 * i + 1];
+    }
+    const auto r = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, 1.0f);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) out[i] = r[i];
+  }
+}
+
+// The value of an E2M1 / E2M3 code (its low 4 / 6 bits) as fp32.
+template <int FMT>
+__device__ inline float mx_code_value(uint32_t code) {
+  constexpr int kMan = FMT == HIGGS_MX_FP4 ? 1 : 3;
+  const uint32_t mag = code & ((4u << kMan) - 1);
+  // exponent field e and mantissa m: 2^(e-1) (1 + m 2^-kMan), or m 2^-kMan for
+  // e = 0; as an fp32 pattern moved down by 2^126, the subnormal case is one too
+  const float v = __builtin_bit_cast(float, mag << (23 - kMan)) *
+                  __builtin_bit_cast(float, 253u << 23);  // 2^126
+  return (code >> (kMan + 2)) & 1 ? -v : v;
+}
+
+// 16 codes (2 or 3 words, least significant bits first) to fp32 values.
+template <int FMT>
+__device__ inline void mx_decode16(const uint32_t* in, float (&v)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if constexpr (FMT == HIGGS_MX_FP4) {
+      v[i] = mx_code_value<FMT>(in[i / 8] >> (4 * (i % 8)));
+    } else {
+      const int bit = 6 * i, w = bit / 32, s = bit % 32;
+      uint32_t c = in[w] >> s;
+      if (s > 26) c |= in[w + 1] << (32 - s);
+      v[i] = mx_code_value<FMT>(c);
+    }
+  }
+}
+
+__device__ inline float bf16_to_f32(uint32_t b) { return __builtin_bit_cast(float, b << 16); }
+// To nearest, ties to even; a NaN stays one.
+__device__ inline uint32_t f32_to_bf16(float f) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, f);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return (u >> 16) | 0x40u;
+  return (u + 0x7fffu + ((u >> 16) & 1)) >> 16;
+}
+
+}  // namespace higgs

@@ -1,0 +1,756 @@
+// Quantization to the microscaled formats, the way back and the layer error.
+//
+// A block of 32 consecutive values v of a row (rotated first where g > 0, as a
+// HIGGS layer's: H (sigma v) / sqrt(g)) is stored as E = max(floor(log2 max|v|)
+// - 2, -127) and the codes of v 2^-E, rounded to nearest with ties to even and
+// saturated at the format's largest magnitude. Blocks that hold a NaN, an
+// infinity or, rotated, a magnitude of 2^128 or more get scale byte 255 (NaN)
+// and codes 0. The rotation is computed in fp64, for codes are decided at
+// borders: bf16 and fp32 inputs of ordinary range are summed exactly, so the
+// codes are those of the exact rotation.
+//
+// With a rotation, a wavefront takes segments of 1024 values (of g for g =
+// 2048 and 4096): 16 consecutive values per lane, rotated by fwht_rows, which
+// leaves a block in the 16 lanes of a DPP row and two registers. Rows are whole
+// groups there, so the matrix is one run of groups.
+
+#include <algorithm>
+#include <cmath>
+
+#include "mx.h"
+#include "wave_fwht.h"
+
+namespace higgs {
+
+void mx_signs(uint64_t seed, int g, MxSigns* s) {
+  struct Entry {
+    uint64_t seed = 0;
+    int g = 0;
+    MxSigns s;
+  };
+  static thread_local Entry kept[4];
+  static thread_local int next = 0;
+  for (const Entry& e : kept)
+    if (e.g == g && e.seed == seed) {
+      *s = e.s;
+      return;
+    }
+  Entry& e = kept[next];
+  next = (next + 1) % 4;
+  e.g = g;
+  e.seed = seed;
+  for (uint32_t& w : e.s.w) w = 0;
+  for (int j = 0; j < g; ++j)
+    if (rht_sign_negative(seed, uint32_t(j))) e.s.w[j / 32] |= 1u << (j % 32);
+  *s = e.s;
+}
+
+namespace {
+
+constexpr int kWaves = 4;
+// LDS dwords per wave: fwht_rows's scratch, or 1024 fp32 values
+constexpr int kWaveLds = kFwhtRows > 1024 ? kFwhtRows : 1024;
+
+// 16 consecutive values from p (aligned to the type only).
+template <typename InT>
+__device__ inline void load16(const InT* p, float (&v)[16]) {
+  if constexpr (sizeof(InT) == 2) {
+    typedef uint16_t u16x8 __attribute__((ext_vector_type(8), aligned(2)));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u16x8 u = *reinterpret_cast<const u16x8*>(p + 8 * h);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[8 * h + i] = bf16_to_f32(u[i]);
+    }
+  } else {
+    typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const f32x4 u = *reinterpret_cast<const f32x4*>(p + 4 * h);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * h + i] = u[i];
+    }
+  }
+}
+
+template <typename InT>
+__device__ inline float load1(const InT* p) {
+  if constexpr (sizeof(InT) == 2) {
+    return bf16_to_f32(*p);
+  } else {
+    return *p;
+  }
+}
+
+// n values (0 .. 16) from p, zeros behind them.
+template <typename InT>
+__device__ inline void load16_upto(const InT* p, int n, float (&v)[16]) {
+  if (n >= 16) {
+    load16(p, v);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = i < n ? load1(p + i) : 0.f;
+}
+
+template <typename OutT>
+__device__ inline void store16(OutT* p, const float (&v)[16]) {
+  if constexpr (sizeof(OutT) == 2) {
+    typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4_a2 u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        u[i] = f32_to_bf16(v[8 * h + 2 * i]) | f32_to_bf16(v[8 * h + 2 * i + 1]) << 16;
+      *reinterpret_cast<u32x4_a2*>(p + 8 * h) = u;
+    }
+  } else {
+    typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      *reinterpret_cast<f32x4*>(p + 4 * h) =
+          f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+  }
+}
+
+template <typename OutT>
+__device__ inline void store16_upto(OutT* p, int n, const float (&v)[16]) {
+  if (n >= 16) {
+    store16(p, v);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (i < n) {
+      if constexpr (sizeof(OutT) == 2) {
+        p[i] = OutT(f32_to_bf16(v[i]));
+      } else {
+        p[i] = v[i];
+      }
+    }
+}
+
+// Codes of 16 values: 2 (E2M1) or 3 (E2M3) words.
+template <int FMT>
+constexpr int kWords16 = FMT == HIGGS_MX_FP4 ? 2 : 3;
+
+template <int FMT>
+__device__ inline void store_codes16(uint8_t* p, const uint32_t* c) {
+#pragma unroll
+  for (int i = 0; i < kWords16<FMT>; ++i) reinterpret_cast<uint32_t*>(p)[i] = c[i];
+}
+template <int FMT>
+__device__ inline void load_codes16(const uint8_t* p, uint32_t* c) {
+#pragma unroll
+  for (int i = 0; i < kWords16<FMT>; ++i) c[i] = reinterpret_cast<const uint32_t*>(p)[i];
+}
+
+// The scale byte of a block from the largest fp32 or fp64 exponent field of its
+// values (255: NaN or infinity).
+__device__ inline uint32_t scale_byte_f32(uint32_t field) {
+  if (field == 255) return 255;
+  return field < uint32_t(kMxTop) ? 0 : field - kMxTop;
+}
+__device__ inline uint32_t scale_byte_f64(uint32_t field) {
+  if (field >= 1023 + 128) return 255;
+  const int b = int(field) - 1023 + 127 - kMxTop;
+  return uint32_t(b < 0 ? 0 : b);
+}
+__device__ inline uint32_t field_f64(double v) {
+  return uint32_t(__builtin_bit_cast(uint64_t, v) >> 52) & 0x7ff;
+}
+// 2^-E of a scale byte, as a double; 0 for the NaN byte (every code is 0 then).
+__device__ inline double inverse_scale(uint32_t byte) {
+  return byte == 255 ? 0.0
+                     : __builtin_bit_cast(double, uint64_t(1023 + 127 - byte) << 52);
+}
+__device__ inline float odd_scaled(double v, uint32_t byte) {
+  return byte == 255 ? 0.f : mx_odd_f32(v * inverse_scale(byte));
+}
+
+// The butterflies' sum times 1 / sqrt(g); a zero gets the sign + (which one the
+// sum leaves depends on its order).
+__device__ inline double normalised(double v, double root) {
+  return __builtin_fma(v, root, 0.0);
+}
+
+// Place of element n of a segment of 1024 in LDS: runs of 16 permuted so that
+// the four rows of lanes hit distinct banks.
+__device__ inline int lds_place(int n) { return n ^ ((((n >> 6) ^ (n >> 8)) & 3) << 4); }
+
+// Moves 16 fp32 values per lane from fwht_rows's places to 16 consecutive ones
+// per lane through the wave's LDS.
+template <int G>
+__device__ inline void rows_to_lanes(float (&v)[16], float* lds, int lane) {
+  wave_lds_sync();
+#pragma unroll
+  for (int r = 0; r < 16; ++r) lds[lds_place(fwht_rows_lane<G>(lane) + fwht_rows_reg<G>(r))] = v[r];
+  wave_lds_sync();
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  const f32x4* p = reinterpret_cast<const f32x4*>(lds + lds_place(16 * lane));
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const f32x4 u = p[h];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[4 * h + i] = u[i];
+  }
+  wave_lds_sync();
+}
+// And back.
+template <int G>
+__device__ inline void lanes_to_rows(float (&v)[16], float* lds, int lane) {
+  wave_lds_sync();
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  f32x4* p = reinterpret_cast<f32x4*>(lds + lds_place(16 * lane));
+#pragma unroll
+  for (int h = 0; h < 4; ++h) p[h] = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+  wave_lds_sync();
+#pragma unroll
+  for (int r = 0; r < 16; ++r) v[r] = lds[lds_place(fwht_rows_lane<G>(lane) + fwht_rows_reg<G>(r))];
+  wave_lds_sync();
+}
+
+// This lane's 16 sign bits for elements 16 lane .. of a segment of 1024.
+template <int G>
+__device__ inline uint32_t lane_signs(const MxSigns& s, int lane) {
+  const int j = (16 * lane) & (G - 1);
+  return s.w[j >> 5] >> (j & 16);
+}
+
+template <int G>
+__device__ inline void signed_f64(const float (&x)[16], uint32_t neg, double (&v)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = double((neg >> i) & 1 ? -x[i] : x[i]);
+}
+
+// ---- quantization ----
+
+template <int G, int FMT, typename InT>
+__global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht(
+    const InT* __restrict__ w, int64_t total, const MxSigns signs, double root,
+    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kWaveLds];
+  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+  uint32_t* const lds = s_lds[wave];
+  const uint32_t neg = lane_signs<G>(signs, lane);
+  const int64_t segs = (total + 1023) / 1024, step = int64_t(gridDim.x) * kWaves;
+  for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
+    const int64_t at = 1024 * seg + 16 * lane;
+    const bool live = at < total;  // total is a multiple of 64
+    float x[16];
+    if (live) {
+      load16(w + at, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    }
+    double v[16];
+    signed_f64<G>(x, neg, v);
+    fwht_rows<G>(v, lds, lane);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] = normalised(v[r], root);
+    // block b = r / 2: registers 2b and 2b + 1 of the row's 16 lanes
+    uint32_t byte[8];
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+      uint32_t f = max(field_f64(v[2 * b]), field_f64(v[2 * b + 1]));
+      f = max(f, lane_xor_small<1>(f));
+      f = max(f, lane_xor_small<2>(f));
+      f = max(f, lane_xor_small<4>(f));
+      f = max(f, lane_xor_small<8>(f));
+      byte[b] = scale_byte_f64(f);
+    }
+    uint32_t mine = byte[0];
+#pragma unroll
+    for (int b = 1; b < 8; ++b) mine = (lane & 7) == b ? byte[b] : mine;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = odd_scaled(v[r], byte[r / 2]);
+    rows_to_lanes<G>(x, reinterpret_cast<float*>(lds), lane);
+    uint32_t c[kWords16<FMT>];
+    mx_encode16<FMT>(x, c);
+    if (live) store_codes16<FMT>(codes + (at / 16) * (4 * kWords16<FMT>), c);
+    if ((lane & 15) < 8) {
+      int e = fwht_rows_lane<G>(lane & ~15);
+#pragma unroll
+      for (int b = 0; b < 8; ++b) e |= (lane & 7) == b ? fwht_rows_reg<G>(2 * b) : 0;
+      const int64_t first = 1024 * seg + e;
+      if (first < total) scales[first / 32] = uint8_t(mine);
+    }
+  }
+}
+
+// Groups of 2048 and 4096: E consecutive values per lane, one group per wave.
+template <int E, int FMT, typename InT>
+__global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht_long(
+    const InT* __restrict__ w, int64_t total, const MxSigns signs, double root,
+    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+  const int64_t segs = total / (64 * E), step = int64_t(gridDim.x) * kWaves;
+  for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
+    const int64_t at = 64 * E * seg + E * lane;
+    double v[E];
+#pragma unroll
+    for (int q = 0; q < E / 16; ++q) {
+      float x[16];
+      load16(w + at + 16 * q, x);
+      const int j = E * lane + 16 * q;
+      const uint32_t neg = signs.w[j >> 5] >> (j & 16);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[16 * q + i] = double((neg >> i) & 1 ? -x[i] : x[i]);
+    }
+    fwht_wave<E>(v, lane, 64 * E);
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = normalised(v[i], root);
+#pragma unroll
+    for (int b = 0; b < E / 32; ++b) {
+      uint32_t f = 0;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) f = max(f, field_f64(v[32 * b + i]));
+      const uint32_t byte = scale_byte_f64(f);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = odd_scaled(v[32 * b + 16 * h + i], byte);
+        uint32_t c[kWords16<FMT>];
+        mx_encode16<FMT>(x, c);
+        store_codes16<FMT>(codes + (at / 16 + 2 * b + h) * (4 * kWords16<FMT>), c);
+      }
+      scales[at / 32 + b] = uint8_t(byte);
+    }
+  }
+}
+
+// No rotation: a lane takes 16 consecutive values, half a block. units: halves
+// of blocks per row; the last block of a row may end early.
+template <int FMT, typename InT>
+__global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__ w, int64_t rows,
+                                                         int64_t in, int64_t units,
+                                                         uint8_t* __restrict__ codes,
+                                                         uint8_t* __restrict__ scales) {
+  const int64_t total = rows * units, step = int64_t(gridDim.x) * 256;
+  // (total is even, so both halves of a block are in range or neither is)
+  for (int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x; u < total; u += step) {
+    const int64_t row = u / units, k = (u - row * units) * 16;
+    const int64_t left = in - k;
+    float x[16];
+    load16_upto(w + row * in + (left > 0 ? k : 0), int(left < 0 ? 0 : left > 16 ? 16 : left), x);
+    uint32_t f = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f = max(f, __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffffu);
+    f = max(f, lane_xor_small<1>(f));
+    const uint32_t byte = scale_byte_f32(f >> 23);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      x[i] = byte == 255 ? 0.f : __builtin_ldexpf(x[i], 127 - int(byte));
+    uint32_t c[kWords16<FMT>];
+    mx_encode16<FMT>(x, c);
+    store_codes16<FMT>(codes + u * (4 * kWords16<FMT>), c);
+    if ((u & 1) == 0) scales[u / 2] = uint8_t(byte);
+  }
+}
+
+// ---- the way back ----
+
+template <int G, int FMT, typename OutT>
+__global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht(
+    const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t total,
+    const MxSigns signs, double root, OutT* __restrict__ w) {
+  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kWaveLds];
+  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+  uint32_t* const lds = s_lds[wave];
+  const uint32_t neg = lane_signs<G>(signs, lane);
+  const int64_t segs = (total + 1023) / 1024, step = int64_t(gridDim.x) * kWaves;
+  for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
+    const int64_t at = 1024 * seg + 16 * lane;
+    const bool live = at < total;
+    uint32_t c[kWords16<FMT>] = {};
+    float scale = 0.f;
+    if (live) {
+      load_codes16<FMT>(codes + (at / 16) * (4 * kWords16<FMT>), c);
+      scale = mx_scale_value(scales[at / 32]);
+    }
+    float x[16];
+    mx_decode16<FMT>(c, x);
+    double v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = double(x[i]) * double(scale);
+    fwht_rows<G>(v, lds, lane);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = float(v[r] * root);
+    rows_to_lanes<G>(x, reinterpret_cast<float*>(lds), lane);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = (neg >> i) & 1 ? -x[i] : x[i];
+    if (live) store16(w + at, x);
+  }
+}
+
+template <int E, int FMT, typename OutT>
+__global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht_long(
+    const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t total,
+    const MxSigns signs, double root, OutT* __restrict__ w) {
+  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+  const int64_t segs = total / (64 * E), step = int64_t(gridDim.x) * kWaves;
+  for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
+    const int64_t at = 64 * E * seg + E * lane;
+    double v[E];
+#pragma unroll
+    for (int q = 0; q < E / 16; ++q) {
+      uint32_t c[kWords16<FMT>];
+      load_codes16<FMT>(codes + (at / 16 + q) * (4 * kWords16<FMT>), c);
+      const double scale = double(mx_scale_value(scales[(at + 16 * q) / 32]));
+      float x[16];
+      mx_decode16<FMT>(c, x);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[16 * q + i] = double(x[i]) * scale;
+    }
+    fwht_wave<E>(v, lane, 64 * E);
+#pragma unroll
+    for (int q = 0; q < E / 16; ++q) {
+      const int j = E * lane + 16 * q;
+      const uint32_t neg = signs.w[j >> 5] >> (j & 16);
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float f = float(v[16 * q + i] * root);
+        x[i] = (neg >> i) & 1 ? -f : f;
+      }
+      store16(w + at + 16 * q, x);
+    }
+  }
+}
+
+template <int FMT, typename OutT>
+__global__ __launch_bounds__(256) void mx_dequantize_plain(const uint8_t* __restrict__ codes,
+                                                           const uint8_t* __restrict__ scales,
+                                                           int64_t rows, int64_t in, int64_t units,
+                                                           OutT* __restrict__ w) {
+  const int64_t total = rows * units, step = int64_t(gridDim.x) * 256;
+  for (int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x; u < total; u += step) {
+    const int64_t row = u / units, k = (u - row * units) * 16;
+    const int64_t left = in - k;
+    if (left <= 0) continue;  // the second half of a row's last block
+    uint32_t c[kWords16<FMT>];
+    load_codes16<FMT>(codes + u * (4 * kWords16<FMT>), c);
+    const float scale = mx_scale_value(scales[u / 2]);
+    float x[16];
+    mx_decode16<FMT>(c, x);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] *= scale;
+    store16_upto(w + row * in + k, int(left > 16 ? 16 : left), x);
+  }
+}
+
+// ---- layer error ----
+
+// A block per row: err = sum (v - q 2^E)^2 over the (rotated) row and norm =
+// sum w^2, fp64, summed in a fixed order.
+__device__ inline void row_sums(double err, double norm, int lane, int wave, double* row_err) {
+  __shared__ double s_sum[2][kWaves];
+  err = wave_sum(err, lane);
+  norm = wave_sum(norm, lane);
+  if (lane == 0) {
+    s_sum[0][wave] = err;
+    s_sum[1][wave] = norm;
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    double t = 0.0;
+    for (int q = 0; q < kWaves; ++q) t += s_sum[threadIdx.x][q];
+    row_err[2 * int64_t(blockIdx.x) + threadIdx.x] = t;
+  }
+}
+
+template <int G, typename InT>
+__global__ __launch_bounds__(64 * kWaves) void mx_error_rht(
+    const InT* __restrict__ w, int64_t in, const MxSigns signs, double root,
+    const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+    double* __restrict__ row_err) {
+  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kWaveLds];
+  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+  uint32_t* const lds = s_lds[wave];
+  const uint32_t neg = lane_signs<G>(signs, lane);
+  const int64_t row = blockIdx.x;
+  const InT* const wr = w + row * in;
+  const uint8_t* const cr = codes + row * (in / 2);
+  const uint8_t* const sr = scales + row * (in / 32);
+  double err = 0.0, norm = 0.0;
+  for (int64_t k0 = 1024 * wave; k0 < in; k0 += 1024 * kWaves) {
+    const int64_t at = k0 + 16 * lane;
+    const bool live = at < in;
+    float x[16];
+    uint32_t c[2] = {0, 0};
+    float scale = 0.f;
+    if (live) {
+      load16(wr + at, x);
+      load_codes16<HIGGS_MX_FP4>(cr + at / 2, c);
+      scale = mx_scale_value(sr[at / 32]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    }
+    double v[16];
+    signed_f64<G>(x, neg, v);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) norm = __builtin_fma(v[i], v[i], norm);
+    mx_decode16<HIGGS_MX_FP4>(c, x);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] *= scale;
+    fwht_rows<G>(v, lds, lane);
+    lanes_to_rows<G>(x, reinterpret_cast<float*>(lds), lane);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const double d = __builtin_fma(v[r], root, -double(x[r]));
+      err = __builtin_fma(d, d, err);
+    }
+  }
+  row_sums(err, norm, lane, wave, row_err);
+}
+
+template <int E, typename InT>
+__global__ __launch_bounds__(64 * kWaves) void mx_error_rht_long(
+    const InT* __restrict__ w, int64_t in, const MxSigns signs, double root,
+    const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+    double* __restrict__ row_err) {
+  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+  const int64_t row = blockIdx.x;
+  double err = 0.0, norm = 0.0;
+  for (int64_t k0 = 64 * E * wave; k0 < in; k0 += 64 * E * kWaves) {
+    const int64_t at = row * in + k0 + E * lane;
+    double v[E];
+#pragma unroll
+    for (int q = 0; q < E / 16; ++q) {
+      float x[16];
+      load16(w + at + 16 * q, x);
+      const int j = E * lane + 16 * q;
+      const uint32_t neg = signs.w[j >> 5] >> (j & 16);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        v[16 * q + i] = double((neg >> i) & 1 ? -x[i] : x[i]);
+        norm = __builtin_fma(v[16 * q + i], v[16 * q + i], norm);
+      }
+    }
+    fwht_wave<E>(v, lane, 64 * E);
+#pragma unroll
+    for (int q = 0; q < E / 16; ++q) {
+      uint32_t c[2];
+      load_codes16<HIGGS_MX_FP4>(codes + (at + 16 * q) / 2, c);
+      const float scale = mx_scale_value(scales[(at + 16 * q) / 32]);
+      float x[16];
+      mx_decode16<HIGGS_MX_FP4>(c, x);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const double d = __builtin_fma(v[16 * q + i], root, -double(x[i] * scale));
+        err = __builtin_fma(d, d, err);
+      }
+    }
+  }
+  row_sums(err, norm, lane, wave, row_err);
+}
+
+template <typename InT>
+__global__ __launch_bounds__(64 * kWaves) void mx_error_plain(const InT* __restrict__ w,
+                                                              int64_t in, int64_t units,
+                                                              const uint8_t* __restrict__ codes,
+                                                              const uint8_t* __restrict__ scales,
+                                                              double* __restrict__ row_err) {
+  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+  const int64_t row = blockIdx.x;
+  double err = 0.0, norm = 0.0;
+  for (int64_t u = threadIdx.x; u < units; u += 64 * kWaves) {
+    const int64_t left = in - 16 * u;
+    if (left <= 0) continue;
+    const int n = int(left > 16 ? 16 : left);
+    float x[16], q[16];
+    load16_upto(w + row * in + 16 * u, n, x);
+    uint32_t c[2];
+    load_codes16<HIGGS_MX_FP4>(codes + (row * units + u) * 8, c);
+    const float scale = mx_scale_value(scales[(row * units + u) / 2]);
+    mx_decode16<HIGGS_MX_FP4>(c, q);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i < n) {
+        const double v = double(x[i]), d = v - double(q[i] * scale);
+        norm = __builtin_fma(v, v, norm);
+        err = __builtin_fma(d, d, err);
+      }
+  }
+  row_sums(err, norm, lane, wave, row_err);
+}
+
+__global__ __launch_bounds__(1024) void mx_t2(const double* __restrict__ row_err, int64_t rows,
+                                              double* __restrict__ t2) {
+  __shared__ double s_sum[2][16];
+  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
+  double err = 0.0, norm = 0.0;
+  for (int64_t r = threadIdx.x; r < rows; r += 1024) {
+    err += row_err[2 * r];
+    norm += row_err[2 * r + 1];
+  }
+  err = wave_sum(err, lane);
+  norm = wave_sum(norm, lane);
+  if (lane == 0) {
+    s_sum[0][wave] = err;
+    s_sum[1][wave] = norm;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double e = 0.0, n = 0.0;
+    for (int q = 0; q < 16; ++q) {
+      e += s_sum[0][q];
+      n += s_sum[1][q];
+    }
+    t2[0] = n == 0.0 ? 0.0 : e / n;
+  }
+}
+
+// Blocks for `waves` wavefronts of work, four to a block: at most eight blocks
+// per compute unit, the kernels loop over the rest.
+unsigned wave_blocks(int64_t waves) {
+  return unsigned(std::min<int64_t>((waves + kWaves - 1) / kWaves, 2048));
+}
+unsigned unit_blocks(int64_t units) {
+  return unsigned(std::min<int64_t>((units + 255) / 256, 1 << 20));
+}
+
+// Calls f(std::integral_constant<int, G>) for the group size.
+template <typename F>
+void for_group(int g, F f) {
+  switch (g) {
+    case 64: f(std::integral_constant<int, 64>{}); break;
+    case 128: f(std::integral_constant<int, 128>{}); break;
+    case 256: f(std::integral_constant<int, 256>{}); break;
+    case 512: f(std::integral_constant<int, 512>{}); break;
+    case 1024: f(std::integral_constant<int, 1024>{}); break;
+    case 2048: f(std::integral_constant<int, 2048>{}); break;
+    default: f(std::integral_constant<int, 4096>{}); break;
+  }
+}
+
+template <int FMT, typename InT>
+hipError_t quantize_typed(const InT* w, int64_t rows, int64_t in, int g, uint64_t seed,
+                          uint8_t* codes, uint8_t* scales, hipStream_t stream) {
+  if (g == 0) {
+    const int64_t units = 2 * mx_blocks(in);
+    hipLaunchKernelGGL((mx_quantize_plain<FMT, InT>), dim3(unit_blocks(rows * units)), dim3(256),
+                       0, stream, w, rows, in, units, codes, scales);
+    return hipGetLastError();
+  }
+  MxSigns signs;
+  mx_signs(seed, g, &signs);
+  const double root = 1.0 / std::sqrt(double(g));
+  const int64_t total = rows * in;
+  for_group(g, [&](auto G) {
+    constexpr int kG = decltype(G)::value;
+    if constexpr (kG <= 1024) {
+      hipLaunchKernelGGL((mx_quantize_rht<kG, FMT, InT>), dim3(wave_blocks((total + 1023) / 1024)),
+                         dim3(64 * kWaves), 0, stream, w, total, signs, root, codes, scales);
+    } else {
+      hipLaunchKernelGGL((mx_quantize_rht_long<kG / 64, FMT, InT>),
+                         dim3(wave_blocks(total / kG)), dim3(64 * kWaves), 0, stream, w, total,
+                         signs, root, codes, scales);
+    }
+  });
+  return hipGetLastError();
+}
+
+template <int FMT, typename OutT>
+hipError_t dequantize_typed(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t in,
+                            int g, uint64_t seed, OutT* w, hipStream_t stream) {
+  if (g == 0) {
+    const int64_t units = 2 * mx_blocks(in);
+    hipLaunchKernelGGL((mx_dequantize_plain<FMT, OutT>), dim3(unit_blocks(rows * units)),
+                       dim3(256), 0, stream, codes, scales, rows, in, units, w);
+    return hipGetLastError();
+  }
+  MxSigns signs;
+  mx_signs(seed, g, &signs);
+  const double root = 1.0 / std::sqrt(double(g));
+  const int64_t total = rows * in;
+  for_group(g, [&](auto G) {
+    constexpr int kG = decltype(G)::value;
+    if constexpr (kG <= 1024) {
+      hipLaunchKernelGGL((mx_dequantize_rht<kG, FMT, OutT>),
+                         dim3(wave_blocks((total + 1023) / 1024)), dim3(64 * kWaves), 0, stream,
+                         codes, scales, total, signs, root, w);
+    } else {
+      hipLaunchKernelGGL((mx_dequantize_rht_long<kG / 64, FMT, OutT>),
+                         dim3(wave_blocks(total / kG)), dim3(64 * kWaves), 0, stream, codes,
+                         scales, total, signs, root, w);
+    }
+  });
+  return hipGetLastError();
+}
+
+template <typename InT>
+hipError_t error_typed(const InT* w, int64_t out, int64_t in, const uint8_t* codes,
+                       const uint8_t* scales, int g, uint64_t seed, double* row_err,
+                       hipStream_t stream) {
+  const dim3 grid{unsigned(out)}, block{64 * kWaves};
+  if (g == 0) {
+    hipLaunchKernelGGL((mx_error_plain<InT>), grid, block, 0, stream, w, in, 2 * mx_blocks(in),
+                       codes, scales, row_err);
+    return hipGetLastError();
+  }
+  MxSigns signs;
+  mx_signs(seed, g, &signs);
+  const double root = 1.0 / std::sqrt(double(g));
+  for_group(g, [&](auto G) {
+    constexpr int kG = decltype(G)::value;
+    if constexpr (kG <= 1024) {
+      hipLaunchKernelGGL((mx_error_rht<kG, InT>), grid, block, 0, stream, w, in, signs, root,
+                         codes, scales, row_err);
+    } else {
+      hipLaunchKernelGGL((mx_error_rht_long<kG / 64, InT>), grid, block, 0, stream, w, in, signs,
+                         root, codes, scales, row_err);
+    }
+  });
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_mx_quantize(const void* w, higgs_dtype dtype, int64_t rows, int64_t in, int fmt,
+                              int g, uint64_t seed, uint8_t* codes, uint8_t* scales,
+                              hipStream_t stream) {
+  const float* wf = static_cast<const float*>(w);
+  const uint16_t* wb = static_cast<const uint16_t*>(w);
+  if (fmt == HIGGS_MX_FP4)
+    return dtype == HIGGS_F32
+               ? quantize_typed<HIGGS_MX_FP4>(wf, rows, in, g, seed, codes, scales, stream)
+               : quantize_typed<HIGGS_MX_FP4>(wb, rows, in, g, seed, codes, scales, stream);
+  return dtype == HIGGS_F32
+             ? quantize_typed<HIGGS_MX_FP6>(wf, rows, in, g, seed, codes, scales, stream)
+             : quantize_typed<HIGGS_MX_FP6>(wb, rows, in, g, seed, codes, scales, stream);
+}
+
+hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows,
+                                int64_t in, int fmt, int g, uint64_t seed, void* w,
+                                higgs_dtype dtype, hipStream_t stream) {
+  float* wf = static_cast<float*>(w);
+  uint16_t* wb = static_cast<uint16_t*>(w);
+  if (fmt == HIGGS_MX_FP4)
+    return dtype == HIGGS_F32
+               ? dequantize_typed<HIGGS_MX_FP4>(codes, scales, rows, in, g, seed, wf, stream)
+               : dequantize_typed<HIGGS_MX_FP4>(codes, scales, rows, in, g, seed, wb, stream);
+  return dtype == HIGGS_F32
+             ? dequantize_typed<HIGGS_MX_FP6>(codes, scales, rows, in, g, seed, wf, stream)
+             : dequantize_typed<HIGGS_MX_FP6>(codes, scales, rows, in, g, seed, wb, stream);
+}
+
+hipError_t launch_mx_layer_error(const void* w, higgs_dtype dtype, int64_t out, int64_t in,
+                                 const uint8_t* codes, const uint8_t* scales, int g, uint64_t seed,
+                                 double* row_err, double* t2, hipStream_t stream) {
+  const hipError_t st =
+      dtype == HIGGS_F32
+          ? error_typed(static_cast<const float*>(w), out, in, codes, scales, g, seed, row_err,
+                        stream)
+          : error_typed(static_cast<const uint16_t*>(w), out, in, codes, scales, g, seed, row_err,
+                        stream);
+  if (st != hipSuccess || t2 == nullptr) return st;
+  hipLaunchKernelGGL(mx_t2, dim3(1), dim3(1024), 0, stream, row_err, out, t2);
+  return hipGetLastError();
+}
+
+}  // namespace higgs

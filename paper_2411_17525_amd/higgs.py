@@ -19,6 +19,8 @@ LIB_PATH = os.environ.get("HIGGS_LIB") or os.path.join(_PKG, "libhiggs.so")
 
 HIGGS_F32 = 0
 HIGGS_BF16 = 1
+MX_FP4 = 0  # higgs_mx_format
+MX_FP6 = 1
 SUPPORTED_GRIDS = ((1, 16), (1, 256), (2, 64), (2, 256), (2, 1024))
 
 _lib = None
@@ -89,6 +91,21 @@ def lib() -> ctypes.CDLL:
     L.higgs_qmatmul_fused_multi.restype = i32
     L.higgs_qmatmul_fused_multi_workspace_bytes.argtypes = [i32, i64, vp, i64, i32, i32, i32]
     L.higgs_qmatmul_fused_multi_workspace_bytes.restype = i64
+    L.higgs_mx_codes_row_bytes.argtypes = [i64, i32]
+    L.higgs_mx_codes_row_bytes.restype = i64
+    L.higgs_mx_scales_row_bytes.argtypes = [i64]
+    L.higgs_mx_scales_row_bytes.restype = i64
+    L.higgs_mx_quantize.argtypes = [vp, i32, i64, i64, i32, i32, u64, vp, vp, vp]
+    L.higgs_mx_quantize.restype = i32
+    L.higgs_mx_dequantize.argtypes = [vp, vp, i64, i64, i32, i32, u64, vp, i32, vp]
+    L.higgs_mx_dequantize.restype = i32
+    L.higgs_mx_layer_error.argtypes = [vp, i32, i64, i64, vp, vp, i32, u64, vp, vp, vp]
+    L.higgs_mx_layer_error.restype = i32
+    L.higgs_mx_qmatmul_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+    L.higgs_mx_qmatmul_workspace_bytes.restype = i64
+    L.higgs_mx_qmatmul.argtypes = [vp, i32, i64, i32, vp, vp, i32, u64, i64, i64, vp, i32, vp, i64,
+                                   vp]
+    L.higgs_mx_qmatmul.restype = i32
     _lib = L
     return L
 
@@ -158,6 +175,17 @@ def _multi_workspace(batch, outs, inp, p, n, g):
     arr = (ctypes.c_int64 * max(len(outs), 1))(*outs)
     return int(lib().higgs_qmatmul_fused_multi_workspace_bytes(len(outs), batch, arr, inp, p, n,
                                                                g))
+
+
+@functools.lru_cache(maxsize=4096)
+def _mx_row_bytes(inp, fmt):
+    """(bytes of a row of codes, of a row of scales) of the microscaled formats."""
+    return int(lib().higgs_mx_codes_row_bytes(inp, fmt)), int(lib().higgs_mx_scales_row_bytes(inp))
+
+
+@functools.lru_cache(maxsize=4096)
+def _mx_workspace(batch, out, inp, fmt, g):
+    return int(lib().higgs_mx_qmatmul_workspace_bytes(batch, out, inp, fmt, g))
 
 
 def _of_sizes(kept, *sizes):
@@ -513,6 +541,153 @@ def qmatmul_fused_multi(x, layers, grid, g: int, ys=None, workspace=None, stream
     return ys
 
 
+# ---------------------------------------------------------------------------
+# microscaled layers (blocks of 32 values with one power of two each)
+# ---------------------------------------------------------------------------
+
+def mx_codes_row_bytes(inp: int, fmt: int = MX_FP4) -> int:
+    return _of_sizes(_mx_row_bytes, inp, fmt)[0]
+
+
+def mx_scales_row_bytes(inp: int) -> int:
+    return _of_sizes(_mx_row_bytes, inp, MX_FP4)[1]
+
+
+def mx_qmatmul_workspace_bytes(batch: int, out: int, inp: int, fmt: int = MX_FP6,
+                               g: int = 0) -> int:
+    return _of_sizes(_mx_workspace, batch, out, inp, fmt, g)
+
+
+def _need_matrix(name, t, dtypes):
+    _need_cuda(name, t, dtypes)
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+
+
+def _need_beside(like, **tensors):
+    """Every tensor given on like's device."""
+    for name, t in tensors.items():
+        if t is not None and t.device != like.device:
+            raise ValueError(f"{name} must be on {like.device}, like the input")
+
+
+def _need_mx_layer(codes, scales, rows, inp, fmt):
+    _need_cuda("codes", codes, _U8)
+    _need_cuda("scales", scales, _U8)
+    cb, sb = _of_sizes(_mx_row_bytes, inp, fmt)
+    if codes.numel() < rows * cb or scales.numel() < rows * sb:
+        raise ValueError(f"codes or scales too small for {rows} rows of {inp}")
+
+
+def _mx_dtype(dtype):
+    if dtype is None:
+        return _torch.float32
+    if dtype not in _FLOATS:
+        raise ValueError(f"dtype must be in {_FLOATS}, got {dtype}")
+    return dtype
+
+
+def _new(like, rows, cols, dtype):
+    t = like.new_empty((rows, cols), dtype=dtype)
+    if type(t) is not _torch.Tensor:
+        t = _torch.empty((rows, cols), dtype=dtype, device=like.device)
+    return t
+
+
+def mx_quantize(w, fmt: int = MX_FP4, g: int = 0, seed: int = 0, codes=None, scales=None,
+                stream=None):
+    """Blocks of 32 values as MX_FP4 (weights, activations) or MX_FP6 (activations)
+    codes with one exponent byte each. w: [rows, in] float32 or bfloat16; g: groups
+    of the rotation, 0 for none.
+
+    Returns (codes uint8 [rows, row_bytes], scales uint8 [rows, ceil(in/32)])."""
+    _need_torch()
+    _need_matrix("w", w, _FLOATS)
+    rows, inp = w.shape
+    cb, sb = _of_sizes(_mx_row_bytes, inp, fmt)
+    if cb < 0:
+        raise HiggsError(1, f"invalid row of in={inp}, format {fmt}")
+    codes = _new(w, rows, cb, _torch.uint8) if codes is None else codes
+    scales = _new(w, rows, sb, _torch.uint8) if scales is None else scales
+    _need_mx_layer(codes, scales, rows, inp, fmt)
+    _need_beside(w, codes=codes, scales=scales)
+    _check(lib().higgs_mx_quantize(_ptr(w), _dtype_code(w), rows, inp, fmt, g, seed, _ptr(codes),
+                                   _ptr(scales), _stream(stream)))
+    return codes, scales
+
+
+def mx_dequantize(codes, scales, in_features: int, fmt: int = MX_FP4, g: int = 0, seed: int = 0,
+                  dtype=None, out=None, stream=None):
+    """The stored values [rows, in_features] (g = 0), or rotated back to the original
+    space (g and seed as quantized), in float32 (default) or bfloat16."""
+    _need_torch()
+    _need_matrix("codes", codes, _U8)
+    rows = codes.shape[0]
+    dtype = _mx_dtype(out.dtype if dtype is None and out is not None else dtype)
+    _need_mx_layer(codes, scales, rows, in_features, fmt)
+    if out is None:
+        out = _new(codes, rows, in_features, dtype)
+    _need_cuda("out", out, (dtype,))
+    if out.numel() < rows * in_features:
+        raise ValueError("out buffer too small")
+    _need_beside(codes, scales=scales, out=out)
+    _check(lib().higgs_mx_dequantize(_ptr(codes), _ptr(scales), rows, in_features, fmt, g, seed,
+                                     _ptr(out), _dtype_code(out), _stream(stream)))
+    return out
+
+
+def mx_layer_error(w, codes, scales, g: int = 0, seed: int = 0, row_err=None, t2=None,
+                   stream=None):
+    """[err, norm] per row of an MX_FP4 layer and its t^2 on the GPU (fp64 device
+    tensors [out, 2] and [1]). Returns (t2 as a float, row_err); reading t2
+    synchronises the stream."""
+    _need_torch()
+    _need_matrix("w", w, _FLOATS)
+    out, inp = w.shape
+    _need_mx_layer(codes, scales, out, inp, MX_FP4)
+    f64 = (_torch.float64,)
+    row_err = _new(w, out, 2, _torch.float64) if row_err is None else row_err
+    t2 = _torch.empty(1, dtype=_torch.float64, device=w.device) if t2 is None else t2
+    _need_cuda("row_err", row_err, f64)
+    _need_cuda("t2", t2, f64)
+    if row_err.numel() < 2 * out or t2.numel() < 1:
+        raise ValueError("row_err or t2 buffer too small")
+    _need_beside(w, codes=codes, scales=scales, row_err=row_err, t2=t2)
+    _check(lib().higgs_mx_layer_error(_ptr(w), _dtype_code(w), out, inp, _ptr(codes), _ptr(scales),
+                                      g, seed, _ptr(row_err), _ptr(t2), _stream(stream)))
+    if stream is not None:
+        stream.synchronize()
+    return float(t2.item()), row_err
+
+
+def mx_qmatmul(x, codes, scales, fmt: int, g: int, seed: int, out_features: int, y=None,
+               workspace=None, dtype=None, stream=None):
+    """y = x_hat W_hat^T of an MX_FP4 layer from raw activations x: [batch, in] float32
+    or bfloat16, which the call rotates (g > 0) and converts to fmt (MX_FP6 or MX_FP4).
+    y is float32 (default) or bfloat16."""
+    _need_torch()
+    _need_matrix("x", x, _FLOATS)
+    batch, inp = x.shape
+    _need_mx_layer(codes, scales, out_features, inp, MX_FP4)
+    dtype = _mx_dtype(y.dtype if dtype is None and y is not None else dtype)
+    if y is None:
+        y = _new(x, batch, out_features, dtype)
+    else:
+        _need_cuda("y", y, (dtype,))
+        if y.numel() < batch * out_features:
+            raise ValueError("y buffer too small")
+    own = workspace is None
+    workspace, ws_ptr, ws_bytes = _workspace(
+        workspace, _of_sizes(_mx_workspace, batch, out_features, inp, fmt, g), x)
+    _need_beside(x, codes=codes, scales=scales, y=y, workspace=workspace)
+    if own and workspace is not None and stream is not None:
+        workspace.record_stream(stream)  # given back to the allocator only after the call's work
+    _check(lib().higgs_mx_qmatmul(_ptr(x), _dtype_code(x), batch, fmt, _ptr(codes), _ptr(scales),
+                                  g, seed, out_features, inp, _ptr(y), _dtype_code(y), ws_ptr,
+                                  ws_bytes, _stream(stream)))
+    return y
+
+
 @dataclasses.dataclass
 class QuantizedLinear:
     """A HIGGS-quantized linear layer: codes, scales, grid, group size and rotation seed."""
@@ -539,3 +714,36 @@ class QuantizedLinear:
         """Same output through the separate rotation and product calls."""
         x_rot = rht_activations(x, self.g, self.seed, out=x_rot)
         return qmatmul(x_rot, self.codes, self.scales, self.grid, self.g, self.out_features, y=y)
+
+
+@dataclasses.dataclass
+class MXLinear:
+    """A linear layer in MX_FP4 blocks: codes, scales, group size (0: no rotation) and
+    seed of the rotation, and the format its activations are converted to."""
+
+    codes: object
+    scales: object
+    g: int
+    seed: int
+    out_features: int
+    in_features: int
+    x_fmt: int = MX_FP6
+
+    @classmethod
+    def from_weight(cls, w, g: int, seed: int, x_fmt: int = MX_FP6):
+        codes, scales = mx_quantize(w, MX_FP4, g, seed)
+        return cls(codes, scales, g, seed, w.shape[0], w.shape[1], x_fmt)
+
+    def forward(self, x, y=None, workspace=None, dtype=None):
+        """y = x_hat W_hat^T (rotation and conversion of x inside the call)."""
+        return mx_qmatmul(x, self.codes, self.scales, self.x_fmt, self.g, self.seed,
+                          self.out_features, y=y, workspace=workspace, dtype=dtype)
+
+    def weight(self, dtype=None):
+        """W_hat [out, in] in the original space."""
+        return mx_dequantize(self.codes, self.scales, self.in_features, MX_FP4, self.g, self.seed,
+                             dtype=dtype)
+
+    def error(self, w):
+        """t^2 = ||W - W_hat||^2 / ||W||^2 (an entry of allocate_bits's table)."""
+        return mx_layer_error(w, self.codes, self.scales, self.g, self.seed)[0]
