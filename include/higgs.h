@@ -503,7 +503,7 @@ int64_t higgs_mx_scales_row_bytes(int64_t in);
  *   codes   [out] device, rows * higgs_mx_codes_row_bytes(in, fmt) bytes,
  *                 16-byte aligned.
  *   scales  [out] device, rows * higgs_mx_scales_row_bytes(in) bytes.
- * Requires rows >= 1, in >= 1, rows * in < 2^40. */
+ * Requires rows >= 1, in >= 1, rows * in <= 2^40. */
 higgs_status higgs_mx_quantize(const void *W, higgs_dtype w_dtype, int64_t rows, int64_t in,
                                higgs_mx_format fmt, int g, uint64_t rht_seed, uint8_t *codes,
                                uint8_t *scales, void *stream);
@@ -548,8 +548,8 @@ higgs_status higgs_mx_layer_error(const void *W, higgs_dtype w_dtype, int64_t ou
  *                    higgs_mx_qmatmul_workspace_bytes(...) bytes, 256-byte
  *                    aligned (may be NULL when that is 0); not preserved. Calls
  *                    that overlap in time need workspaces of their own.
- * Requires batch >= 1, out >= 1, in >= 1, batch * in < 2^40, in <= 2^20,
- * codes below 2 GiB (HIGGS_ERR_UNSUPPORTED otherwise). */
+ * Requires batch >= 1, out >= 1, in >= 1, batch * in <= 2^36, batch * out <=
+ * 2^40, in <= 2^20, codes below 2 GiB (HIGGS_ERR_UNSUPPORTED otherwise). */
 int64_t higgs_mx_qmatmul_workspace_bytes(int64_t batch, int64_t out, int64_t in,
                                          higgs_mx_format x_fmt, int g);
 higgs_status higgs_mx_qmatmul(const void *x, higgs_dtype x_dtype, int64_t batch,

@@ -551,6 +551,8 @@ higgs_status check_mx_product(int64_t batch, int64_t out, int64_t in, int fmt, i
   // the kernels address codes with 32-bit byte offsets
   if (out * higgs::mx_blocks(in) * 16 >= (int64_t(1) << 31))
     return fail(HIGGS_ERR_UNSUPPORTED, "layer too large: codes must be < 2 GiB");
+  if (batch > (int64_t(1) << 36) / in)
+    return fail(HIGGS_ERR_UNSUPPORTED, "batch * in must be below 2^36");
   if (batch > (int64_t(1) << 40) / out)
     return fail(HIGGS_ERR_UNSUPPORTED, "batch * out must be below 2^40");
   return HIGGS_OK;

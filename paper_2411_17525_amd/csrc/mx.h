@@ -24,10 +24,31 @@ struct MxSigns {
 // (mx_quant.hip; computed once per seed and group size, kept per thread)
 void mx_signs(uint64_t seed, int g, MxSigns* s);
 
+// Activations in the product's order, so that what a wave loads of a stage (128
+// values of K) is consecutive: per 32 rows and stage, two halves (64 values) of
+// 64 units, unit l = block l / 32 of row l % 32; 16 bytes per unit, and for
+// E2M3 the blocks' last 8 bytes behind the half's 64 first parts. The scale
+// bytes of a stage's four blocks as a word per row: [stage][rows32].
+struct MxTiles {
+  uint8_t* codes;
+  uint8_t* scales;
+  int64_t stages;  // of a row: ceil(in / 128), zeros behind `in`
+  int64_t rows32;  // rows, rounded up to whole tiles of 32
+};
+constexpr int mx_half_bytes(int fmt) { return fmt == HIGGS_MX_FP4 ? 1024 : 1536; }
+// Offset of the half (1 or 1.5 KiB) that holds block kb of a row.
+template <int FMT>
+__host__ __device__ inline int64_t mx_tile_unit(const MxTiles& t, uint32_t row, uint32_t kb) {
+  return ((int64_t(row / 32) * t.stages + kb / 4) * 2 + kb / 2 % 2) * mx_half_bytes(FMT);
+}
+
 // Kernel launchers. g = 0: no rotation. The arguments have been checked.
 hipError_t launch_mx_quantize(const void* w, higgs_dtype dtype, int64_t rows, int64_t in, int fmt,
                               int g, uint64_t seed, uint8_t* codes, uint8_t* scales,
                               hipStream_t stream);
+// The same into the product's order (one launch; batch * in < 2^36).
+hipError_t launch_mx_tiles(const void* x, higgs_dtype dtype, int64_t batch, int64_t in, int fmt,
+                           int g, uint64_t seed, const MxTiles& tiles, hipStream_t stream);
 hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows,
                                 int64_t in, int fmt, int g, uint64_t seed, void* w,
                                 higgs_dtype dtype, hipStream_t stream);

@@ -16,6 +16,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "mx.h"
 #include "wave_fwht.h"
@@ -146,6 +147,65 @@ __device__ inline void load_codes16(const uint8_t* p, uint32_t* c) {
   for (int i = 0; i < kWords16<FMT>; ++i) c[i] = reinterpret_cast<const uint32_t*>(p)[i];
 }
 
+// Where a quantizer's kernel puts half-block u of the matrix (16 codes) and block
+// u's scale byte, u counted along the rows: the caller's arrays, row after row.
+struct RowSink {
+  uint8_t* codes;
+  uint8_t* scales;
+  template <int FMT>
+  __device__ void put(int64_t u, const uint32_t* c) const {
+    store_codes16<FMT>(codes + u * (4 * kWords16<FMT>), c);
+  }
+  __device__ void put_scale(int64_t u, uint32_t byte) const { scales[u] = uint8_t(byte); }
+};
+
+// The same into the product's layout (MxTiles). Rows of `halves` half-blocks (a
+// multiple of 4 with a rotation), u below 2^32.
+struct TileSink {
+  MxTiles t;
+  uint32_t halves;
+  template <int FMT>
+  __device__ void put_at(uint32_t row, uint32_t k, const uint32_t* c) const {
+    uint8_t* const unit = t.codes + mx_tile_unit<FMT>(t, row, k >> 1);
+    uint8_t* const head = unit + (row % 32 + (k >> 1) % 2 * 32) * 16;
+    if constexpr (FMT == HIGGS_MX_FP4) {
+      *reinterpret_cast<uint2*>(head + (k & 1) * 8) = make_uint2(c[0], c[1]);
+    } else {
+      // a block's 24 bytes are 16 and 8 apart: 12 of the first half, 4 + 8
+      uint32_t* const tail =
+          reinterpret_cast<uint32_t*>(unit + 1024 + (row % 32 + (k >> 1) % 2 * 32) * 8);
+      uint32_t* const h = reinterpret_cast<uint32_t*>(head);
+      if ((k & 1) == 0) {
+        h[0] = c[0];
+        h[1] = c[1];
+        h[2] = c[2];
+      } else {
+        h[3] = c[0];
+        tail[0] = c[1];
+        tail[1] = c[2];
+      }
+    }
+  }
+  __device__ void put_scale_at(uint32_t row, uint32_t kb, uint32_t byte) const {
+    t.scales[(int64_t(kb >> 2) * t.rows32 + row) * 4 + (kb & 3)] = uint8_t(byte);
+  }
+  template <int FMT>
+  __device__ void put(int64_t u, const uint32_t* c) const {
+    const uint32_t row = uint32_t(u) / halves, k = uint32_t(u) - row * halves;
+    put_at<FMT>(row, k, c);
+    // a row of 2 blocks more than whole stages: zeros up to the stage's end
+    if (k + 4 >= halves && ((halves >> 1) & 3) == 2) {
+      const uint32_t zero[3] = {0, 0, 0};
+      put_at<FMT>(row, k + 4, zero);
+    }
+  }
+  __device__ void put_scale(int64_t u, uint32_t byte) const {
+    const uint32_t blocks = halves >> 1, row = uint32_t(u) / blocks, kb = uint32_t(u) - row * blocks;
+    put_scale_at(row, kb, byte);
+    if (kb + 2 >= blocks && (blocks & 3) == 2) put_scale_at(row, kb + 2, 0);
+  }
+};
+
 // The scale byte of a block from the largest fp32 or fp64 exponent field of its
 // values (255: NaN or infinity).
 __device__ inline uint32_t scale_byte_f32(uint32_t field) {
@@ -226,10 +286,9 @@ __device__ inline void signed_f64(const float (&x)[16], uint32_t neg, double (&v
 
 // ---- quantization ----
 
-template <int G, int FMT, typename InT>
+template <int G, int FMT, typename InT, typename Sink>
 __global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht(
-    const InT* __restrict__ w, int64_t total, const MxSigns signs, double root,
-    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    const InT* __restrict__ w, int64_t total, const MxSigns signs, double root, const Sink sink) {
   __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kWaveLds];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
   uint32_t* const lds = s_lds[wave];
@@ -269,22 +328,21 @@ __global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht(
     rows_to_lanes<G>(x, reinterpret_cast<float*>(lds), lane);
     uint32_t c[kWords16<FMT>];
     mx_encode16<FMT>(x, c);
-    if (live) store_codes16<FMT>(codes + (at / 16) * (4 * kWords16<FMT>), c);
+    if (live) sink.template put<FMT>(at / 16, c);
     if ((lane & 15) < 8) {
       int e = fwht_rows_lane<G>(lane & ~15);
 #pragma unroll
       for (int b = 0; b < 8; ++b) e |= (lane & 7) == b ? fwht_rows_reg<G>(2 * b) : 0;
       const int64_t first = 1024 * seg + e;
-      if (first < total) scales[first / 32] = uint8_t(mine);
+      if (first < total) sink.put_scale(first / 32, mine);
     }
   }
 }
 
 // Groups of 2048 and 4096: E consecutive values per lane, one group per wave.
-template <int E, int FMT, typename InT>
+template <int E, int FMT, typename InT, typename Sink>
 __global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht_long(
-    const InT* __restrict__ w, int64_t total, const MxSigns signs, double root,
-    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    const InT* __restrict__ w, int64_t total, const MxSigns signs, double root, const Sink sink) {
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
   const int64_t segs = total / (64 * E), step = int64_t(gridDim.x) * kWaves;
   for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
@@ -315,20 +373,20 @@ __global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht_long(
         for (int i = 0; i < 16; ++i) x[i] = odd_scaled(v[32 * b + 16 * h + i], byte);
         uint32_t c[kWords16<FMT>];
         mx_encode16<FMT>(x, c);
-        store_codes16<FMT>(codes + (at / 16 + 2 * b + h) * (4 * kWords16<FMT>), c);
+        sink.template put<FMT>(at / 16 + 2 * b + h, c);
       }
-      scales[at / 32 + b] = uint8_t(byte);
+      sink.put_scale(at / 32 + b, byte);
     }
   }
 }
 
 // No rotation: a lane takes 16 consecutive values, half a block. units: halves
-// of blocks per row; the last block of a row may end early.
-template <int FMT, typename InT>
+// of blocks per row; the last block of a row may end early, and blocks behind it
+// (the product's layout has whole stages) are zeros.
+template <int FMT, typename InT, typename Sink>
 __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__ w, int64_t rows,
                                                          int64_t in, int64_t units,
-                                                         uint8_t* __restrict__ codes,
-                                                         uint8_t* __restrict__ scales) {
+                                                         const Sink sink) {
   const int64_t total = rows * units, step = int64_t(gridDim.x) * 256;
   // (total is even, so both halves of a block are in range or neither is)
   for (int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x; u < total; u += step) {
@@ -346,8 +404,13 @@ __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__
       x[i] = byte == 255 ? 0.f : __builtin_ldexpf(x[i], 127 - int(byte));
     uint32_t c[kWords16<FMT>];
     mx_encode16<FMT>(x, c);
-    store_codes16<FMT>(codes + u * (4 * kWords16<FMT>), c);
-    if ((u & 1) == 0) scales[u / 2] = uint8_t(byte);
+    if constexpr (std::is_same_v<Sink, TileSink>) {
+      sink.template put_at<FMT>(uint32_t(row), uint32_t(u - row * units), c);
+      if ((u & 1) == 0) sink.put_scale_at(uint32_t(row), uint32_t(u - row * units) >> 1, byte);
+    } else {
+      sink.template put<FMT>(u, c);
+      if ((u & 1) == 0) sink.put_scale(u / 2, byte);
+    }
   }
 }
 
@@ -628,13 +691,13 @@ void for_group(int g, F f) {
   }
 }
 
-template <int FMT, typename InT>
-hipError_t quantize_typed(const InT* w, int64_t rows, int64_t in, int g, uint64_t seed,
-                          uint8_t* codes, uint8_t* scales, hipStream_t stream) {
+// units: half-blocks per row that the sink holds.
+template <int FMT, typename InT, typename Sink>
+hipError_t quantize_typed(const InT* w, int64_t rows, int64_t in, int64_t units, int g,
+                          uint64_t seed, const Sink& sink, hipStream_t stream) {
   if (g == 0) {
-    const int64_t units = 2 * mx_blocks(in);
-    hipLaunchKernelGGL((mx_quantize_plain<FMT, InT>), dim3(unit_blocks(rows * units)), dim3(256),
-                       0, stream, w, rows, in, units, codes, scales);
+    hipLaunchKernelGGL((mx_quantize_plain<FMT, InT, Sink>), dim3(unit_blocks(rows * units)),
+                       dim3(256), 0, stream, w, rows, in, units, sink);
     return hipGetLastError();
   }
   MxSigns signs;
@@ -644,12 +707,13 @@ hipError_t quantize_typed(const InT* w, int64_t rows, int64_t in, int g, uint64_
   for_group(g, [&](auto G) {
     constexpr int kG = decltype(G)::value;
     if constexpr (kG <= 1024) {
-      hipLaunchKernelGGL((mx_quantize_rht<kG, FMT, InT>), dim3(wave_blocks((total + 1023) / 1024)),
-                         dim3(64 * kWaves), 0, stream, w, total, signs, root, codes, scales);
+      hipLaunchKernelGGL((mx_quantize_rht<kG, FMT, InT, Sink>),
+                         dim3(wave_blocks((total + 1023) / 1024)), dim3(64 * kWaves), 0, stream, w,
+                         total, signs, root, sink);
     } else {
-      hipLaunchKernelGGL((mx_quantize_rht_long<kG / 64, FMT, InT>),
+      hipLaunchKernelGGL((mx_quantize_rht_long<kG / 64, FMT, InT, Sink>),
                          dim3(wave_blocks(total / kG)), dim3(64 * kWaves), 0, stream, w, total,
-                         signs, root, codes, scales);
+                         signs, root, sink);
     }
   });
   return hipGetLastError();
@@ -711,18 +775,32 @@ hipError_t error_typed(const InT* w, int64_t out, int64_t in, const uint8_t* cod
 
 }  // namespace
 
-hipError_t launch_mx_quantize(const void* w, higgs_dtype dtype, int64_t rows, int64_t in, int fmt,
-                              int g, uint64_t seed, uint8_t* codes, uint8_t* scales,
-                              hipStream_t stream) {
+template <typename Sink>
+static hipError_t quantize_any(const void* w, higgs_dtype dtype, int64_t rows, int64_t in,
+                               int64_t units, int fmt, int g, uint64_t seed, const Sink& sink,
+                               hipStream_t stream) {
   const float* wf = static_cast<const float*>(w);
   const uint16_t* wb = static_cast<const uint16_t*>(w);
   if (fmt == HIGGS_MX_FP4)
     return dtype == HIGGS_F32
-               ? quantize_typed<HIGGS_MX_FP4>(wf, rows, in, g, seed, codes, scales, stream)
-               : quantize_typed<HIGGS_MX_FP4>(wb, rows, in, g, seed, codes, scales, stream);
+               ? quantize_typed<HIGGS_MX_FP4>(wf, rows, in, units, g, seed, sink, stream)
+               : quantize_typed<HIGGS_MX_FP4>(wb, rows, in, units, g, seed, sink, stream);
   return dtype == HIGGS_F32
-             ? quantize_typed<HIGGS_MX_FP6>(wf, rows, in, g, seed, codes, scales, stream)
-             : quantize_typed<HIGGS_MX_FP6>(wb, rows, in, g, seed, codes, scales, stream);
+             ? quantize_typed<HIGGS_MX_FP6>(wf, rows, in, units, g, seed, sink, stream)
+             : quantize_typed<HIGGS_MX_FP6>(wb, rows, in, units, g, seed, sink, stream);
+}
+
+hipError_t launch_mx_quantize(const void* w, higgs_dtype dtype, int64_t rows, int64_t in, int fmt,
+                              int g, uint64_t seed, uint8_t* codes, uint8_t* scales,
+                              hipStream_t stream) {
+  return quantize_any(w, dtype, rows, in, 2 * mx_blocks(in), fmt, g, seed,
+                      RowSink{codes, scales}, stream);
+}
+
+hipError_t launch_mx_tiles(const void* x, higgs_dtype dtype, int64_t batch, int64_t in, int fmt,
+                           int g, uint64_t seed, const MxTiles& tiles, hipStream_t stream) {
+  return quantize_any(x, dtype, batch, in, g == 0 ? 8 * tiles.stages : 2 * mx_blocks(in), fmt, g,
+                      seed, TileSink{tiles, uint32_t(in / 16)}, stream);
 }
 
 hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows,
