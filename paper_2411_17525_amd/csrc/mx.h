@@ -139,11 +139,10 @@ __device__ inline void mx_decode16(const uint32_t* in, float (&v)[16]) {
 }
 
 __device__ inline float bf16_to_f32(uint32_t b) { return __builtin_bit_cast(float, b << 16); }
-// To nearest, ties to even; a NaN stays one.
-__device__ inline uint32_t f32_to_bf16(float f) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, f);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return (u >> 16) | 0x40u;
-  return (u + 0x7fffu + ((u >> 16) & 1)) >> 16;
+// Two values to bf16 in one word, to nearest with ties to even (one instruction).
+__device__ inline uint32_t pack_bf16(float lo, float hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, bf16x2{__bf16(lo), __bf16(hi)});
 }
 
 }  // namespace higgs

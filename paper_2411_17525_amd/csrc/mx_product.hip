@@ -37,8 +37,6 @@ struct Args {
   int mtiles, ntiles;
 };
 
-constexpr int kBufs = 3;  // stages in LDS
-
 template <int N>
 __device__ inline void wait_vm() {
   // vmcnt <= N, the other counters free
@@ -49,15 +47,31 @@ __device__ inline __amdgpu_buffer_rsrc_t rsrc(const void* p, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, int(bytes), 0x00020000);
 }
 
+// All of the wave's LDS reads have arrived, then all waves of the block meet.
+__device__ inline void wait_lds_and_meet() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// f(0), f(1), ... f(N - 1) with constants.
+template <int N, int I = 0, typename F>
+__device__ MX_INLINE inline void for_each(const F& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    for_each<N, I + 1>(f);
+  }
+}
+
 // A block computes BM activation rows x BN outputs over a range of K with WM x WN
 // waves, stage by stage of 128 values: the stage's activations, weights and scale
-// words go from memory to LDS (kBufs stages; the loads run two and a half stages
+// words go from memory to LDS (BUFS stages; the loads run BUFS - 1/2 stages
 // ahead), from there into the operands. A stage is computed in halves; the
 // operands of a half are read while the other half is multiplied, and the one
 // barrier of a stage stands between its halves: there the next stage has landed
 // and this one has been read by all waves.
-template <int BM, int BN, int WM, int WN, int FMT, typename OutT>
-__global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a) {
+template <int BM, int BN, int WM, int WN, int BUFS, int PERCU, int FMT, typename OutT>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_tiles(
+    const Args a) {
+  constexpr int kBufs = BUFS;
   constexpr int kWaves = WM * WN;
   constexpr int kHalf = mx_half_bytes(FMT), kTile = 2 * kHalf;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
@@ -71,7 +85,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
   constexpr int kXPer = (kXLoads + kWaves - 1) / kWaves, kWPer = (kWLoads + kWaves - 1) / kWaves;
   constexpr int kSPer = (kSLoads + kWaves - 1) / kWaves;
   constexpr int kLoads = kXPer + kWPer + kSPer;
-  static_assert(BM % 64 == 0 && BN % 64 == 0 && kBufs * kStage <= 160 * 1024, "tile");
+  static_assert(BM % 64 == 0 && BN % 64 == 0 && PERCU * kBufs * kStage <= 160 * 1024, "tile");
   __shared__ __attribute__((aligned(1024))) uint8_t s_mem[kBufs * kStage];
 
   const int tid = int(threadIdx.x), lane = tid & 63;
@@ -98,11 +112,17 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
   // ---- loads of a stage ----
   const int mrows = int(min(int64_t(BM), a.x.rows32 - m0));   // a multiple of 32
   const int nrows = int(min(int64_t(BN), a.out - n0));
-  const __amdgpu_buffer_rsrc_t xrs =
-      rsrc(a.x.codes + m0 / 32 * stages * kTile, uint32_t(mrows / 32 * stages * kTile));
-  const __amdgpu_buffer_rsrc_t wrs = rsrc(a.wc + n0 * a.blocks * 16, uint32_t(nrows * a.blocks * 16));
-  const __amdgpu_buffer_rsrc_t xss = rsrc(a.x.scales + m0 * 4, uint32_t(((stages - 1) * a.x.rows32 + mrows) * 4));
-  const __amdgpu_buffer_rsrc_t wss = rsrc(a.ws + n0 * a.ws_pitch, uint32_t(nrows * a.ws_pitch));
+  // sizes in bytes of what the block may read; 0 for the loads of stages past the
+  // end, which then read nothing (every stage issues the same number of loads, for
+  // the waits count them)
+  const uint8_t* const xp = a.x.codes + m0 / 32 * stages * kTile;
+  const uint8_t* const wp = a.wc + n0 * a.blocks * 16;
+  const uint8_t* const xsp = a.x.scales + m0 * 4;
+  const uint8_t* const wsp = a.ws + n0 * a.ws_pitch;
+  const uint32_t xbytes = uint32_t(mrows / 32 * stages * kTile);
+  const uint32_t wbytes = uint32_t(nrows * a.blocks * 16);
+  const uint32_t xsbytes = uint32_t(((stages - 1) * a.x.rows32 + mrows) * 4);
+  const uint32_t wsbytes = uint32_t(nrows * a.ws_pitch);
   uint32_t xoff[kXPer], woff[kWPer], soff[kSPer];
 #pragma unroll
   for (int i = 0; i < kXPer; ++i) {
@@ -126,58 +146,79 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
     else
       soff[i] = uint32_t(min((j - BM / 64) * 64 + lane, nrows - 1) * a.ws_pitch + first * 4);
   }
-  auto issue = [&](int buf) MX_INLINE {
+  // load k of this wave (constant) into buffer buf, and its offset one stage on
+  auto issue = [&](auto K, int buf, bool live) MX_INLINE {
+    constexpr int k = decltype(K)::value;
     uint8_t* const s = s_mem + buf * kStage;
-#pragma unroll
-    for (int i = 0; i < kXPer; ++i) {
-      const int j = min(wave + i * kWaves, kXLoads - 1);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(xrs, (lds_void*)(s + j * 1024), 16, int(xoff[i]), 0,
-                                               0, 0);
-      xoff[i] += kTile;
-    }
-#pragma unroll
-    for (int i = 0; i < kWPer; ++i) {
+    if constexpr (k < kXPer) {
+      const int j = min(wave + k * kWaves, kXLoads - 1);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(xp, live ? xbytes : 0), (lds_void*)(s + j * 1024),
+                                               16, int(xoff[k]), 0, 0, 0);
+      xoff[k] += kTile;
+    } else if constexpr (k < kXPer + kWPer) {
+      constexpr int i = k - kXPer;
       const int j = min(wave + i * kWaves, kWLoads - 1);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(wrs, (lds_void*)(s + kXBytes + j * 1024), 16,
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(wp, live ? wbytes : 0),
+                                               (lds_void*)(s + kXBytes + j * 1024), 16,
                                                int(woff[i]), 0, 0, 0);
       woff[i] += 64;
-    }
-#pragma unroll
-    for (int i = 0; i < kSPer; ++i) {
+    } else {
+      constexpr int i = k - kXPer - kWPer;
       const int j = min(wave + i * kWaves, kSLoads - 1);
       const bool is_x = j < BM / 64;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(is_x ? xss : wss, (lds_void*)(s + kXScale + j * 256),
-                                               4, int(soff[i]), 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rsrc(is_x ? xsp : wsp, live ? is_x ? xsbytes : wsbytes : 0),
+          (lds_void*)(s + kXScale + j * 256), 4, int(soff[i]), 0, 0, 0);
       soff[i] += is_x ? uint32_t(a.x.rows32 * 4) : 4u;
     }
   };
 
   // ---- operands of half h of the stage in buffer buf ----
   struct Half {
-    i32x8 x[TM], w[TN];
-    int xs[TM], ws[TN];
+    uint32_t x[TM][6], w[TN][4];
+    uint32_t xs[TM], ws[TN];
   };
-  auto read = [&](Half& f, int buf, int h) MX_INLINE {
+  // (the tails' addresses apart: two of them read by one instruction would have to
+  // be moved into place)
+  uint32_t tail[TM];
+#pragma unroll
+  for (int m = 0; m < TM; ++m) {
+    tail[m] = uint32_t((wm * TM + m) * kTile + 1024 + lane * 8);
+    asm volatile("" : "+v"(tail[m]));
+  }
+  // read k of a half's operands, in the order in which the products need them:
+  // the first row tile, all column tiles, the other row tiles
+  constexpr int kXReads = FMT == HIGGS_MX_FP6 ? 3 : 2;
+  constexpr int kReads = TM * kXReads + TN * 2;
+  auto read = [&](auto K, Half& f, int buf, int h) MX_INLINE {
+    constexpr int k = decltype(K)::value;
     const uint8_t* const s = s_mem + buf * kStage;
-#pragma unroll
-    for (int m = 0; m < TM; ++m) {
-      const uint8_t* const p = s + (wm * TM + m) * kTile + h * kHalf;
-      const u32x4 u = *reinterpret_cast<const u32x4*>(p + lane * 16);
-      f.x[m] = i32x8{int(u[0]), int(u[1]), int(u[2]), int(u[3]), 0, 0, 0, 0};
-      if constexpr (FMT == HIGGS_MX_FP6) {
-        const u32x2 v = *reinterpret_cast<const u32x2*>(p + 1024 + lane * 8);
-        f.x[m][4] = int(v[0]);
-        f.x[m][5] = int(v[1]);
-      }
-      f.xs[m] = *reinterpret_cast<const int*>(s + kXScale + ((wm * TM + m) * 32 + r32) * 4);
-    }
-#pragma unroll
-    for (int n = 0; n < TN; ++n) {
+    if constexpr (k >= kXReads && k < kXReads + TN * 2) {
+      constexpr int n = (k - kXReads) / 2;
       const int row = (wn * TN + n) * 32 + r32;
-      const int unit = (2 * h + hi) ^ ((row >> 1) & 3);
-      const u32x4 u = *reinterpret_cast<const u32x4*>(s + kXBytes + row * 64 + unit * 16);
-      f.w[n] = i32x8{int(u[0]), int(u[1]), int(u[2]), int(u[3]), 0, 0, 0, 0};
-      f.ws[n] = *reinterpret_cast<const int*>(s + kWScale + row * 4);
+      if constexpr ((k - kXReads) % 2 == 0) {
+        const int unit = (2 * h + hi) ^ ((row >> 1) & 3);
+        const u32x4 u = *reinterpret_cast<const u32x4*>(s + kXBytes + row * 64 + unit * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f.w[n][i] = u[i];
+      } else {
+        f.ws[n] = *reinterpret_cast<const uint32_t*>(s + kWScale + row * 4);
+      }
+    } else {
+      constexpr int q = k < kXReads ? k : k - TN * 2, m = q / kXReads, part = q % kXReads;
+      if constexpr (part == 0) {
+        const u32x4 u =
+            *reinterpret_cast<const u32x4*>(s + (wm * TM + m) * kTile + h * kHalf + lane * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f.x[m][i] = u[i];
+      } else if constexpr (part == 1) {
+        f.xs[m] =
+            *reinterpret_cast<const uint32_t*>(s + kXScale + ((wm * TM + m) * 32 + r32) * 4);
+      } else {
+        const u32x2 u = *reinterpret_cast<const u32x2*>(s + tail[m] + h * kHalf);
+        f.x[m][4] = u[0];
+        f.x[m][5] = u[1];
+      }
     }
   };
   f32x16 acc[TM][TN];
@@ -185,73 +226,125 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
   for (int m = 0; m < TM; ++m)
 #pragma unroll
     for (int n = 0; n < TN; ++n) acc[m][n] = f32x16{};
-  auto multiply = [&](const Half& f, auto H) MX_INLINE {
-    constexpr int h = decltype(H)::value;  // its scale is byte 2 h + lane / 32 of the word
-    constexpr int kFormat = FMT == HIGGS_MX_FP4 ? 4 : 2;
-    int xs[TM], ws[TN];
-#pragma unroll
-    for (int m = 0; m < TM; ++m) xs[m] = int(uint32_t(f.xs[m]) >> (8 * hi));
-#pragma unroll
-    for (int n = 0; n < TN; ++n) ws[n] = int(uint32_t(f.ws[n]) >> (8 * hi));
-#pragma unroll
-    for (int m = 0; m < TM; ++m)
-#pragma unroll
-      for (int n = 0; n < TN; ++n)
-        acc[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-            f.x[m], f.w[n], acc[m][n], kFormat, 4, 2 * h, xs[m], 2 * h, ws[n]);
+  // product k of a half; the scale bytes of half h are byte 2 h + lane / 32 of the words
+  auto multiply = [&](auto K, const Half& f, auto H) MX_INLINE {
+    constexpr int m = decltype(K)::value / TN, n = decltype(K)::value % TN;
+    constexpr int h = decltype(H)::value, kFormat = FMT == HIGGS_MX_FP4 ? 4 : 2;
+    const i32x8 x = {int(f.x[m][0]), int(f.x[m][1]), int(f.x[m][2]), int(f.x[m][3]),
+                     FMT == HIGGS_MX_FP6 ? int(f.x[m][4]) : 0,
+                     FMT == HIGGS_MX_FP6 ? int(f.x[m][5]) : 0, 0, 0};
+    const i32x8 w = {int(f.w[n][0]), int(f.w[n][1]), int(f.w[n][2]), int(f.w[n][3]), 0, 0, 0, 0};
+    acc[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+        x, w, acc[m][n], kFormat, 4, 2 * h, int(f.xs[m] >> (8 * hi)), 2 * h,
+        int(f.ws[n] >> (8 * hi)));
   };
   using H0 = std::integral_constant<int, 0>;
   using H1 = std::integral_constant<int, 1>;
 
-  for (int t = 0; t < min(kBufs, count); ++t) issue(t);
+  // One half of a stage: its products, behind each a share of the reads of the
+  // half that comes next (done by three quarters of the products) and of the loads
+  // [L0, L1) (spread over all: a wave that issues several at a time waits for the
+  // address unit, and its products wait behind them). The order is kept as written.
+  constexpr int kProducts = TM * TN;
+  auto half = [&](const Half& now, auto H, Half& next, int nbuf, int nh, auto L0, auto L1,
+                  int lbuf, bool live) MX_INLINE {
+    constexpr int kOver = kProducts >= 4 ? kProducts * 3 / 4 : kProducts;
+    constexpr int l0 = decltype(L0)::value, nl = decltype(L1)::value - l0;
+    for_each<kProducts>([&](auto I) MX_INLINE {
+      constexpr int i = decltype(I)::value;
+      multiply(I, now, H);
+      constexpr int ra = kReads * (i < kOver ? i : kOver) / kOver;
+      constexpr int rb = kReads * (i + 1 < kOver ? i + 1 : kOver) / kOver;
+      for_each<rb - ra>([&](auto J) MX_INLINE {
+        read(std::integral_constant<int, ra + decltype(J)::value>{}, next, nbuf, nh);
+      });
+      constexpr int la = l0 + nl * i / kProducts, lb = l0 + nl * (i + 1) / kProducts;
+      for_each<lb - la>([&](auto J) MX_INLINE {
+        issue(std::integral_constant<int, la + decltype(J)::value>{}, lbuf, live);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  using L0 = std::integral_constant<int, 0>;
+  using LH = std::integral_constant<int, (kLoads + 1) / 2>;
+  using LN = std::integral_constant<int, kLoads>;
+
+  // Stage 0 .. kBufs - 2 and the first half of the loads of kBufs - 1: what the
+  // loop has issued where a stage begins.
+  for (int t = 0; t < kBufs - 1; ++t)
+    for_each<kLoads>([&](auto K) MX_INLINE { issue(K, t, t < count); });
+  for_each<LH::value>([&](auto K) MX_INLINE { issue(K, kBufs - 1, kBufs - 1 < count); });
+  wait_vm<(kBufs - 2) * kLoads + LH::value>();
+  wait_lds_and_meet();
   Half f0, f1;
-  if (count >= kBufs)
-    wait_vm<2 * kLoads>();
-  else
-    wait_vm<0>();
-  __syncthreads();
-  read(f0, 0, 0);
-  int buf = 0;
+  for_each<kReads>([&](auto K) MX_INLINE { read(K, f0, 0, 0); });
+  // One stage: half 0, the meeting, half 1. From the meeting on the loads of stage
+  // t + kBufs go into this stage's buffer, the first half of them in half 1 and the
+  // others in half 0 of stage t + 1. At the meeting the loads of kBufs - 2 stages
+  // behind the next one may be outstanding.
+  int buf = 0, before = kBufs - 1;
   for (int t = 0; t < count; ++t) {
     const int next = buf == kBufs - 1 ? 0 : buf + 1;
-    read(f1, buf, 1);
-    multiply(f0, H0{});
-    // the next stage's loads are the oldest but kLoads (stage t + 2); the last
-    // stages just wait for all
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (t + 2 < count)
-      wait_vm<kLoads>();
-    else
-      wait_vm<0>();
-    asm volatile("s_barrier" ::: "memory");
-    if (t + kBufs < count) issue(buf);
-    read(f0, next, 0);
-    multiply(f1, H1{});
+    __builtin_amdgcn_sched_barrier(0);
+    half(f0, H0{}, f1, buf, 1, LH{}, LN{}, before, t + kBufs - 1 < count);
+    wait_vm<(kBufs - 2) * kLoads>();
+    wait_lds_and_meet();
+    __builtin_amdgcn_sched_barrier(0);
+    half(f1, H1{}, f0, next, 0, L0{}, LH{}, buf, t + kBufs < count);
+    before = buf;
     buf = next;
   }
+  wait_vm<0>();
 
-  // ---- outputs ----
+  // ---- outputs: register i holds row i % 4 + 8 (i / 4) + 4 hi, column r32 ----
   const bool partial = a.splits > 1;
-  const int64_t bw = m0 + wm * TM * 32 + 4 * hi, ow = n0 + wn * TN * 32 + r32;
-  const int64_t at = (partial ? split * a.batch * a.out : 0) + bw * a.out + ow;
-  const int brows = int(min(a.batch - bw, int64_t(BM))), ocols = int(min(a.out - ow, int64_t(BN)));
-  float* const yf = static_cast<float*>(a.y) + at;
-  uint16_t* const yb = static_cast<uint16_t*>(a.y) + at;
+  const int64_t bw = m0 + wm * TM * 32, ow = n0 + wn * TN * 32;
+  const int brows = int(min(a.batch - bw, int64_t(BM))) - 4 * hi;
+  const int ocols = int(min(a.out - ow, int64_t(BN))) - r32;
+  const bool full = a.batch - bw >= TM * 32 && a.out - ow >= TN * 32;
+  if (sizeof(OutT) == 4 || partial) {
+    float* const y = static_cast<float*>(a.y) + (partial ? split * a.batch * a.out : 0) +
+                     bw * a.out + ow;
+    const uint32_t lane_at = uint32_t(4 * hi) * uint32_t(a.out) + uint32_t(r32);
 #pragma unroll
-  for (int m = 0; m < TM; ++m)
+    for (int m = 0; m < TM; ++m)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int b = m * 32 + i % 4 + 8 * (i / 4);
-      const int64_t row = b * a.out;
+      for (int i = 0; i < 16; ++i) {
+        const int b = m * 32 + i % 4 + 8 * (i / 4);
 #pragma unroll
-      for (int n = 0; n < TN; ++n)
-        if (b < brows && n * 32 < ocols) {
-          if (sizeof(OutT) == 4 || partial)
-            yf[row + n * 32] = acc[m][n][i];
-          else
-            yb[row + n * 32] = uint16_t(f32_to_bf16(acc[m][n][i]));
+        for (int n = 0; n < TN; ++n)
+          if (full || (b < brows && n * 32 < ocols))
+            y[b * a.out + n * 32 + lane_at] = acc[m][n][i];
+      }
+  } else {
+    // two rows of a column per word; lanes 2 j and 2 j + 1 exchange them to two
+    // columns of a row, lane 2 j storing the first row and lane 2 j + 1 the second
+    uint16_t* const y = static_cast<uint16_t*>(a.y) + bw * a.out + ow;
+    const int odd = lane & 1;
+    const bool pairs = full && a.out % 2 == 0;
+    const uint32_t lane_at = uint32_t(4 * hi + odd) * uint32_t(a.out) + uint32_t(r32 - odd);
+    const uint32_t each_at = uint32_t(4 * hi) * uint32_t(a.out) + uint32_t(r32);
+#pragma unroll
+    for (int m = 0; m < TM; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const int b = m * 32 + i % 4 + 8 * (i / 4);
+#pragma unroll
+        for (int n = 0; n < TN; ++n) {
+          const uint32_t v = pack_bf16(acc[m][n][i], acc[m][n][i + 1]);
+          if (pairs) {
+            const uint32_t p = lane_xor_small<1>(v);
+            // even: (own low, partner's low); odd: (partner's high, own high)
+            const uint32_t w = odd ? __builtin_amdgcn_perm(v, p, 0x07060302u)
+                                   : __builtin_amdgcn_perm(p, v, 0x05040100u);
+            *reinterpret_cast<uint32_t*>(y + b * a.out + n * 32 + lane_at) = w;
+          } else if (n * 32 < ocols) {
+            if (b < brows) y[b * a.out + n * 32 + each_at] = uint16_t(v);
+            if (b + 1 < brows) y[(b + 1) * a.out + n * 32 + each_at] = uint16_t(v >> 16);
+          }
         }
-    }
+      }
+  }
 }
 
 // Rows of scale bytes to a pitch of whole words, zeros behind the row.
@@ -288,12 +381,12 @@ Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt) {
   return p;
 }
 
-template <int BM, int BN, int WM, int WN, int FMT, typename OutT>
+template <int BM, int BN, int WM, int WN, int BUFS, int PERCU, int FMT, typename OutT>
 hipError_t launch_tiles(Args a, hipStream_t stream) {
   a.mtiles = int((a.batch + BM - 1) / BM);
   a.ntiles = int((a.out + BN - 1) / BN);
   a.splits = 1;
-  const auto kernel = mx_product_tiles<BM, BN, WM, WN, FMT, OutT>;
+  const auto kernel = mx_product_tiles<BM, BN, WM, WN, BUFS, PERCU, FMT, OutT>;
   hipLaunchKernelGGL(kernel, dim3(unsigned(a.mtiles * a.ntiles * a.splits)), dim3(64 * WM * WN),
                      0, stream, a);
   return hipGetLastError();
@@ -335,11 +428,11 @@ hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, 
   }
   if (fmt == HIGGS_MX_FP4)
     return y_dtype == HIGGS_F32
-               ? launch_tiles<256, 256, 2, 2, HIGGS_MX_FP4, float>(a, stream)
-               : launch_tiles<256, 256, 2, 2, HIGGS_MX_FP4, uint16_t>(a, stream);
+               ? launch_tiles<256, 256, 4, 2, 3, 1, HIGGS_MX_FP4, float>(a, stream)
+               : launch_tiles<256, 256, 4, 2, 3, 1, HIGGS_MX_FP4, uint16_t>(a, stream);
   return y_dtype == HIGGS_F32
-             ? launch_tiles<256, 256, 2, 2, HIGGS_MX_FP6, float>(a, stream)
-             : launch_tiles<256, 256, 2, 2, HIGGS_MX_FP6, uint16_t>(a, stream);
+             ? launch_tiles<256, 256, 4, 2, 3, 1, HIGGS_MX_FP6, float>(a, stream)
+             : launch_tiles<256, 256, 4, 2, 3, 1, HIGGS_MX_FP6, uint16_t>(a, stream);
 }
 
 }  // namespace higgs

@@ -103,7 +103,7 @@ __device__ inline void store16(OutT* p, const float (&v)[16]) {
       u32x4_a2 u;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        u[i] = f32_to_bf16(v[8 * h + 2 * i]) | f32_to_bf16(v[8 * h + 2 * i + 1]) << 16;
+        u[i] = pack_bf16(v[8 * h + 2 * i], v[8 * h + 2 * i + 1]);
       *reinterpret_cast<u32x4_a2*>(p + 8 * h) = u;
     }
   } else {
@@ -125,7 +125,7 @@ __device__ inline void store16_upto(OutT* p, int n, const float (&v)[16]) {
   for (int i = 0; i < 16; ++i)
     if (i < n) {
       if constexpr (sizeof(OutT) == 2) {
-        p[i] = OutT(f32_to_bf16(v[i]));
+        p[i] = OutT(pack_bf16(v[i], 0.f));
       } else {
         p[i] = v[i];
       }
