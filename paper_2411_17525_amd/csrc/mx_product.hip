@@ -28,12 +28,11 @@ typedef __attribute__((address_space(3))) void lds_void;
 struct Args {
   MxTiles x;
   const uint8_t* wc;
-  const uint8_t* ws;
-  void* y;         // or fp32 partial sums [split][batch][out]
+  const uint32_t* ws;  // weight scales, a word per stage and row: [stage][out]
+  void* y;             // or fp32 partial sums [split][batch][out]
   int64_t batch, out;
-  int blocks;      // of a weight row
-  int ws_pitch;    // bytes of a row of weight scales, a multiple of 4
-  int splits;      // of K
+  int blocks;  // of a weight row
+  int splits;  // of K
   int mtiles, ntiles;
 };
 
@@ -63,30 +62,32 @@ __device__ MX_INLINE inline void for_each(const F& f) {
 
 // A block computes BM activation rows x BN outputs over a range of K with WM x WN
 // waves, stage by stage of 128 values: the stage's activations, weights and scale
-// words go from memory to LDS (BUFS stages; the loads run BUFS - 1/2 stages
-// ahead), from there into the operands. A stage is computed in halves; the
+// words go from memory to LDS, from there into the operands. The loads run two and
+// a half stages ahead. Weights are loaded for two stages at a time, 128 bytes of a
+// row: the address unit takes about as long for half a line as for a whole one
+// (62, 88 and 106 GB/s per compute unit in pieces of 64, 128 and 256 bytes), and
+// that time is what the products have to hide. So that every stage loads as much,
+// the block's first half of columns has its pairs of stages at (0, 1), (2, 3) ..,
+// the second at (-1, 0), (1, 2) .. A stage is computed in halves; the
 // operands of a half are read while the other half is multiplied, and the one
 // barrier of a stage stands between its halves: there the next stage has landed
 // and this one has been read by all waves.
-template <int BM, int BN, int WM, int WN, int BUFS, int PERCU, int FMT, typename OutT>
-__global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_tiles(
-    const Args a) {
-  constexpr int kBufs = BUFS;
+template <int BM, int BN, int WM, int WN, int FMT, typename OutT>
+__global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a) {
   constexpr int kWaves = WM * WN;
   constexpr int kHalf = mx_half_bytes(FMT), kTile = 2 * kHalf;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-  constexpr int kXBytes = BM / 32 * kTile, kWBytes = BN * 64;
-  constexpr int kXScale = kXBytes + kWBytes, kWScale = kXScale + BM * 4;
-  constexpr int kStage = kWScale + BN * 4;
+  // LDS: three stages of activations and scale words; of each half of the columns
+  // two pairs of weights
+  constexpr int kXBytes = BM / 32 * kTile, kXScale = kXBytes, kWScale = kXScale + BM * 4;
+  constexpr int kStage = kWScale + BN * 4, kPair = BN / 2 * 128, kWeights = 3 * kStage;
   // loads of 1 KiB (codes) and 256 bytes (scales) per stage, and per wave; a wave
   // without one repeats the last
-  constexpr int kXLoads = kXBytes / 1024, kWLoads = kWBytes / 1024;
-  constexpr int kSLoads = (BM + BN) / 64;
+  constexpr int kXLoads = kXBytes / 1024, kWLoads = kPair / 1024, kSLoads = (BM + BN) / 64;
   constexpr int kXPer = (kXLoads + kWaves - 1) / kWaves, kWPer = (kWLoads + kWaves - 1) / kWaves;
-  constexpr int kSPer = (kSLoads + kWaves - 1) / kWaves;
-  constexpr int kLoads = kXPer + kWPer + kSPer;
-  static_assert(BM % 64 == 0 && BN % 64 == 0 && PERCU * kBufs * kStage <= 160 * 1024, "tile");
-  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[kBufs * kStage];
+  constexpr int kSPer = (kSLoads + kWaves - 1) / kWaves, kLoads = kXPer + kSPer + kWPer;
+  static_assert(BM % 64 == 0 && BN % 64 == 0 && kWeights + 4 * kPair <= 160 * 1024, "tile");
+  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[kWeights + 4 * kPair];
 
   const int tid = int(threadIdx.x), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -115,39 +116,42 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   // sizes in bytes of what the block may read; 0 for the loads of stages past the
   // end, which then read nothing (every stage issues the same number of loads, for
   // the waits count them)
-  const uint8_t* const xp = a.x.codes + m0 / 32 * stages * kTile;
+  const uint8_t* const xp = a.x.codes + (m0 / 32 * stages + first) * kTile;
   const uint8_t* const wp = a.wc + n0 * a.blocks * 16;
-  const uint8_t* const xsp = a.x.scales + m0 * 4;
-  const uint8_t* const wsp = a.ws + n0 * a.ws_pitch;
-  const uint32_t xbytes = uint32_t(mrows / 32 * stages * kTile);
+  const uint8_t* const xsp = a.x.scales + (first * a.x.rows32 + m0) * 4;
+  const uint32_t* const wsp = a.ws + first * a.out + n0;
+  const uint32_t xbytes = uint32_t(((mrows / 32 - 1) * stages + count) * kTile);
   const uint32_t wbytes = uint32_t(nrows * a.blocks * 16);
-  const uint32_t xsbytes = uint32_t(((stages - 1) * a.x.rows32 + mrows) * 4);
-  const uint32_t wsbytes = uint32_t(nrows * a.ws_pitch);
-  uint32_t xoff[kXPer], woff[kWPer], soff[kSPer];
+  const uint32_t xsbytes = uint32_t(((count - 1) * a.x.rows32 + mrows) * 4);
+  const uint32_t wsbytes = uint32_t(((count - 1) * a.out + nrows) * 4);
+  uint32_t xoff[kXPer], woff[2][kWPer], soff[kSPer];  // (woff[0]: of the next stage's half)
 #pragma unroll
   for (int i = 0; i < kXPer; ++i) {
     const int j = min(wave + i * kWaves, kXLoads - 1);
     const int at = j * 1024 + lane * 16, t = min(at / kTile, mrows / 32 - 1);
-    xoff[i] = uint32_t((t * stages + first) * kTile + at % kTile);
+    xoff[i] = uint32_t(t * stages * kTile + at % kTile);
   }
 #pragma unroll
   for (int i = 0; i < kWPer; ++i) {
-    // 16 rows of 64 bytes; a row's four blocks are permuted so that eight rows of
+    // 8 rows of 128 bytes; a row's eight blocks are permuted so that eight rows of
     // one block lie in distinct banks
-    const int row = min(wave + i * kWaves, kWLoads - 1) * 16 + lane / 4;
-    const int unit = (lane & 3) ^ ((row >> 1) & 3);
-    woff[i] = uint32_t(min(row, nrows - 1) * a.blocks * 16 + first * 64 + unit * 16);
+    const int row = min(wave + i * kWaves, kWLoads - 1) * 8 + lane / 8;
+    const int at = first * 64 + ((lane & 7) ^ (row & 7)) * 16;
+    woff[1][i] = uint32_t(min(row, nrows - 1) * a.blocks * 16 + at);
+    // (its first pair begins a stage early: what that reads is not used, below the
+    // buffer's start it is out of range)
+    woff[0][i] = uint32_t(min(row + BN / 2, nrows - 1) * a.blocks * 16 + at - 64);
   }
 #pragma unroll
   for (int i = 0; i < kSPer; ++i) {
     const int j = min(wave + i * kWaves, kSLoads - 1);
-    if (j < BM / 64)
-      soff[i] = uint32_t((int64_t(first) * a.x.rows32 + min(j * 64 + lane, mrows - 1)) * 4);
-    else
-      soff[i] = uint32_t(min((j - BM / 64) * 64 + lane, nrows - 1) * a.ws_pitch + first * 4);
+    soff[i] = j < BM / 64 ? uint32_t(min(j * 64 + lane, mrows - 1) * 4)
+                          : uint32_t(min((j - BM / 64) * 64 + lane, nrows - 1) * 4);
   }
-  // load k of this wave (constant) into buffer buf, and its offset one stage on
-  auto issue = [&](auto K, int buf, bool live) MX_INLINE {
+  // load k of this wave (constant) for stage t into stage buffer buf, and its offset
+  // one stage or pair on; the last weight load hands over to the other columns
+  auto issue = [&](auto K, int t, int buf) MX_INLINE {
+    const bool live = t < count;
     constexpr int k = decltype(K)::value;
     uint8_t* const s = s_mem + buf * kStage;
     if constexpr (k < kXPer) {
@@ -155,21 +159,24 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(xp, live ? xbytes : 0), (lds_void*)(s + j * 1024),
                                                16, int(xoff[k]), 0, 0, 0);
       xoff[k] += kTile;
-    } else if constexpr (k < kXPer + kWPer) {
+    } else if constexpr (k < kXPer + kSPer) {
       constexpr int i = k - kXPer;
-      const int j = min(wave + i * kWaves, kWLoads - 1);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(wp, live ? wbytes : 0),
-                                               (lds_void*)(s + kXBytes + j * 1024), 16,
-                                               int(woff[i]), 0, 0, 0);
-      woff[i] += 64;
-    } else {
-      constexpr int i = k - kXPer - kWPer;
       const int j = min(wave + i * kWaves, kSLoads - 1);
       const bool is_x = j < BM / 64;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rsrc(is_x ? xsp : wsp, live ? is_x ? xsbytes : wsbytes : 0),
+          rsrc(is_x ? static_cast<const void*>(xsp) : wsp, live ? is_x ? xsbytes : wsbytes : 0),
           (lds_void*)(s + kXScale + j * 256), 4, int(soff[i]), 0, 0, 0);
-      soff[i] += is_x ? uint32_t(a.x.rows32 * 4) : 4u;
+      soff[i] += uint32_t(is_x ? a.x.rows32 : a.out) * 4;
+    } else {
+      constexpr int i = k - kXPer - kSPer;
+      const int j = min(wave + i * kWaves, kWLoads - 1);
+      const int pair = (t & 1) * 2 + ((t + (t & 1)) >> 1 & 1);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rsrc(wp, live ? wbytes : 0), (lds_void*)(s_mem + kWeights + pair * kPair + j * 1024), 16,
+          int(woff[0][i]), 0, 0, 0);
+      const uint32_t other = woff[1][i];
+      woff[1][i] = woff[0][i] + 128;
+      woff[0][i] = other;
     }
   };
 
@@ -190,15 +197,19 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   // the first row tile, all column tiles, the other row tiles
   constexpr int kXReads = FMT == HIGGS_MX_FP6 ? 3 : 2;
   constexpr int kReads = TM * kXReads + TN * 2;
-  auto read = [&](auto K, Half& f, int buf, int h) MX_INLINE {
+  auto read = [&](auto K, Half& f, int t, int buf, int h) MX_INLINE {
     constexpr int k = decltype(K)::value;
     const uint8_t* const s = s_mem + buf * kStage;
     if constexpr (k >= kXReads && k < kXReads + TN * 2) {
       constexpr int n = (k - kXReads) / 2;
       const int row = (wn * TN + n) * 32 + r32;
       if constexpr ((k - kXReads) % 2 == 0) {
-        const int unit = (2 * h + hi) ^ ((row >> 1) & 3);
-        const u32x4 u = *reinterpret_cast<const u32x4*>(s + kXBytes + row * 64 + unit * 16);
+        const int side = row / (BN / 2);  // (the same in all lanes)
+        const int pair = __builtin_amdgcn_readfirstlane(side * 2 + ((t + side) >> 1 & 1));
+        const int odd = __builtin_amdgcn_readfirstlane((t + side) & 1);
+        const int unit = (4 * odd + 2 * h + hi) ^ (row & 7);
+        const u32x4 u = *reinterpret_cast<const u32x4*>(
+            s_mem + kWeights + pair * kPair + (row - side * (BN / 2)) * 128 + unit * 16);
 #pragma unroll
         for (int i = 0; i < 4; ++i) f.w[n][i] = u[i];
       } else {
@@ -246,8 +257,8 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   // [L0, L1) (spread over all: a wave that issues several at a time waits for the
   // address unit, and its products wait behind them). The order is kept as written.
   constexpr int kProducts = TM * TN;
-  auto half = [&](const Half& now, auto H, Half& next, int nbuf, int nh, auto L0, auto L1,
-                  int lbuf, bool live) MX_INLINE {
+  auto half = [&](const Half& now, auto H, Half& next, int nt, int nbuf, int nh, auto L0, auto L1,
+                  int lt, int lbuf) MX_INLINE {
     constexpr int kOver = kProducts >= 4 ? kProducts * 3 / 4 : kProducts;
     constexpr int l0 = decltype(L0)::value, nl = decltype(L1)::value - l0;
     for_each<kProducts>([&](auto I) MX_INLINE {
@@ -256,41 +267,41 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
       constexpr int ra = kReads * (i < kOver ? i : kOver) / kOver;
       constexpr int rb = kReads * (i + 1 < kOver ? i + 1 : kOver) / kOver;
       for_each<rb - ra>([&](auto J) MX_INLINE {
-        read(std::integral_constant<int, ra + decltype(J)::value>{}, next, nbuf, nh);
+        read(std::integral_constant<int, ra + decltype(J)::value>{}, next, nt, nbuf, nh);
       });
       constexpr int la = l0 + nl * i / kProducts, lb = l0 + nl * (i + 1) / kProducts;
       for_each<lb - la>([&](auto J) MX_INLINE {
-        issue(std::integral_constant<int, la + decltype(J)::value>{}, lbuf, live);
+        issue(std::integral_constant<int, la + decltype(J)::value>{}, lt, lbuf);
       });
       __builtin_amdgcn_sched_barrier(0);
     });
   };
+  // The loads for stage t + 3 go out from the meeting of stage t on, where their
+  // buffers are free: the first of them in its half 1, the others in half 0 of stage
+  // t + 1. So at the meeting of stage t the loads for stage t + 2 may be outstanding,
+  // those for t + 1 not.
   using L0 = std::integral_constant<int, 0>;
   using LH = std::integral_constant<int, (kLoads + 1) / 2>;
   using LN = std::integral_constant<int, kLoads>;
-
-  // Stage 0 .. kBufs - 2 and the first half of the loads of kBufs - 1: what the
-  // loop has issued where a stage begins.
-  for (int t = 0; t < kBufs - 1; ++t)
-    for_each<kLoads>([&](auto K) MX_INLINE { issue(K, t, t < count); });
-  for_each<LH::value>([&](auto K) MX_INLINE { issue(K, kBufs - 1, kBufs - 1 < count); });
-  wait_vm<(kBufs - 2) * kLoads + LH::value>();
+  for_each<kWPer>([&](auto K) MX_INLINE {  // (the second columns' pair that ends with stage 0)
+    issue(std::integral_constant<int, kXPer + kSPer + decltype(K)::value>{}, -1, 0);
+  });
+  for_each<kLoads>([&](auto K) MX_INLINE { issue(K, 0, 0); });
+  for_each<kLoads>([&](auto K) MX_INLINE { issue(K, 1, 1); });
+  for_each<LH::value>([&](auto K) MX_INLINE { issue(K, 2, 2); });
+  wait_vm<kLoads + LH::value>();
   wait_lds_and_meet();
   Half f0, f1;
-  for_each<kReads>([&](auto K) MX_INLINE { read(K, f0, 0, 0); });
-  // One stage: half 0, the meeting, half 1. From the meeting on the loads of stage
-  // t + kBufs go into this stage's buffer, the first half of them in half 1 and the
-  // others in half 0 of stage t + 1. At the meeting the loads of kBufs - 2 stages
-  // behind the next one may be outstanding.
-  int buf = 0, before = kBufs - 1;
+  for_each<kReads>([&](auto K) MX_INLINE { read(K, f0, 0, 0, 0); });
+  int buf = 0, before = 2;
   for (int t = 0; t < count; ++t) {
-    const int next = buf == kBufs - 1 ? 0 : buf + 1;
+    const int next = buf == 2 ? 0 : buf + 1;
     __builtin_amdgcn_sched_barrier(0);
-    half(f0, H0{}, f1, buf, 1, LH{}, LN{}, before, t + kBufs - 1 < count);
-    wait_vm<(kBufs - 2) * kLoads>();
+    half(f0, H0{}, f1, t, buf, 1, LH{}, LN{}, t + 2, before);
+    wait_vm<kLoads>();
     wait_lds_and_meet();
     __builtin_amdgcn_sched_barrier(0);
-    half(f1, H1{}, f0, next, 0, L0{}, LH{}, buf, t + kBufs < count);
+    half(f1, H1{}, f0, t + 1, next, 0, L0{}, LH{}, t + 3, buf);
     before = buf;
     buf = next;
   }
@@ -347,26 +358,36 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   }
 }
 
-// Rows of scale bytes to a pitch of whole words, zeros behind the row.
-__global__ __launch_bounds__(256) void mx_pad_scales(const uint8_t* __restrict__ s, int64_t rows,
-                                                     int blocks, int pitch,
-                                                     uint32_t* __restrict__ d) {
-  const int words = pitch / 4;
-  const int64_t total = rows * words, step = int64_t(gridDim.x) * 256;
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += step) {
-    const int64_t row = i / words;
-    const int k = int(i - row * words) * 4;
-    uint32_t w = 0;
-    for (int j = 0; j < 4; ++j)
-      if (k + j < blocks) w |= uint32_t(s[row * blocks + k + j]) << (8 * j);
-    d[i] = w;
+// Weight scales, row after row, to words of a stage's four blocks, stage after
+// stage; zeros behind a row's end. A wave reads 16 bytes each of 64 rows and
+// writes four runs of 64 words.
+__global__ __launch_bounds__(256) void mx_scale_words(const uint8_t* __restrict__ s, int64_t rows,
+                                                      int blocks, int stages,
+                                                      uint32_t* __restrict__ d) {
+  const int64_t row = int64_t(blockIdx.x) * 64 + (threadIdx.x & 63);
+  if (row >= rows) return;
+  const uint8_t* const p = s + row * blocks;
+  for (int t0 = (int(blockIdx.y) * 4 + int(threadIdx.x >> 6)) * 4; t0 < stages;
+       t0 += int(gridDim.y) * 16) {
+    if (t0 * 4 + 16 <= blocks) {
+      typedef uint32_t u32x4_a1 __attribute__((ext_vector_type(4), aligned(1)));
+      const u32x4_a1 u = *reinterpret_cast<const u32x4_a1*>(p + t0 * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) d[(t0 + i) * rows + row] = u[i];
+    } else {
+      for (int t = t0; t < min(t0 + 4, stages); ++t) {
+        uint32_t w = 0;
+        for (int j = 0; j < 4; ++j)
+          if (t * 4 + j < blocks) w |= uint32_t(p[t * 4 + j]) << (8 * j);
+        d[t * rows + row] = w;
+      }
+    }
   }
 }
 
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
-// The workspace: activation codes and scales, padded weight scales (only where
-// the caller's have another pitch or alignment).
+// The workspace: activation codes and scales, weight scale words.
 struct Plan {
   int64_t stages, rows32, x_bytes, xs_bytes, ws_bytes;
   int64_t bytes() const { return x_bytes + xs_bytes + ws_bytes; }
@@ -381,12 +402,12 @@ Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt) {
   return p;
 }
 
-template <int BM, int BN, int WM, int WN, int BUFS, int PERCU, int FMT, typename OutT>
+template <int BM, int BN, int WM, int WN, int FMT, typename OutT>
 hipError_t launch_tiles(Args a, hipStream_t stream) {
   a.mtiles = int((a.batch + BM - 1) / BM);
   a.ntiles = int((a.out + BN - 1) / BN);
   a.splits = 1;
-  const auto kernel = mx_product_tiles<BM, BN, WM, WN, BUFS, PERCU, FMT, OutT>;
+  const auto kernel = mx_product_tiles<BM, BN, WM, WN, FMT, OutT>;
   hipLaunchKernelGGL(kernel, dim3(unsigned(a.mtiles * a.ntiles * a.splits)), dim3(64 * WM * WN),
                      0, stream, a);
   return hipGetLastError();
@@ -409,30 +430,25 @@ hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, 
   a.x = MxTiles{w, w + p.x_bytes, p.stages, p.rows32};
   hipError_t st = launch_mx_tiles(x, x_dtype, batch, in, fmt, g, seed, a.x, stream);
   if (st != hipSuccess) return st;
+  uint32_t* const words = reinterpret_cast<uint32_t*>(w + p.x_bytes + p.xs_bytes);
   a.wc = codes;
-  a.ws = scales;
+  a.ws = words;
   a.y = y;
   a.batch = batch;
   a.out = out;
   a.blocks = int(mx_blocks(in));
-  a.ws_pitch = a.blocks;
-  if (a.blocks % 4 != 0 || reinterpret_cast<uintptr_t>(scales) % 4 != 0) {
-    a.ws_pitch = int(p.stages * 4);
-    uint32_t* const d = reinterpret_cast<uint32_t*>(w + p.x_bytes + p.xs_bytes);
-    const int64_t words = out * p.stages;
-    hipLaunchKernelGGL(mx_pad_scales, dim3(unsigned(std::min<int64_t>((words + 255) / 256, 4096))),
-                       dim3(256), 0, stream, scales, out, a.blocks, a.ws_pitch, d);
-    st = hipGetLastError();
-    if (st != hipSuccess) return st;
-    a.ws = reinterpret_cast<const uint8_t*>(d);
-  }
+  hipLaunchKernelGGL(mx_scale_words,
+                     dim3(unsigned((out + 63) / 64), unsigned(std::min<int64_t>((p.stages + 15) / 16, 64))),
+                     dim3(256), 0, stream, scales, out, a.blocks, int(p.stages), words);
+  st = hipGetLastError();
+  if (st != hipSuccess) return st;
   if (fmt == HIGGS_MX_FP4)
     return y_dtype == HIGGS_F32
-               ? launch_tiles<256, 256, 4, 2, 3, 1, HIGGS_MX_FP4, float>(a, stream)
-               : launch_tiles<256, 256, 4, 2, 3, 1, HIGGS_MX_FP4, uint16_t>(a, stream);
+               ? launch_tiles<256, 256, 4, 2, HIGGS_MX_FP4, float>(a, stream)
+               : launch_tiles<256, 256, 4, 2, HIGGS_MX_FP4, uint16_t>(a, stream);
   return y_dtype == HIGGS_F32
-             ? launch_tiles<256, 256, 4, 2, 3, 1, HIGGS_MX_FP6, float>(a, stream)
-             : launch_tiles<256, 256, 4, 2, 3, 1, HIGGS_MX_FP6, uint16_t>(a, stream);
+             ? launch_tiles<256, 256, 4, 2, HIGGS_MX_FP6, float>(a, stream)
+             : launch_tiles<256, 256, 4, 2, HIGGS_MX_FP6, uint16_t>(a, stream);
 }
 
 }  // namespace higgs
