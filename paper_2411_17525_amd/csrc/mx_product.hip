@@ -62,32 +62,36 @@ __device__ MX_INLINE inline void for_each(const F& f) {
 
 // A block computes BM activation rows x BN outputs over a range of K with WM x WN
 // waves, stage by stage of 128 values: the stage's activations, weights and scale
-// words go from memory to LDS, from there into the operands. The loads run two and
-// a half stages ahead. Weights are loaded for two stages at a time, 128 bytes of a
+// words go from memory to LDS, from there into the operands. The loads run NB - 1/2
+// stages ahead. Weights are loaded for two stages at a time, 128 bytes of a
 // row: the address unit takes about as long for half a line as for a whole one
 // (62, 88 and 106 GB/s per compute unit in pieces of 64, 128 and 256 bytes), and
 // that time is what the products have to hide. So that every stage loads as much,
 // the block's first half of columns has its pairs of stages at (0, 1), (2, 3) ..,
-// the second at (-1, 0), (1, 2) .. A stage is computed in halves; the
+// the second at (-1, 0), (1, 2) .. (NB is odd). A stage is computed in halves; the
 // operands of a half are read while the other half is multiplied, and the one
 // barrier of a stage stands between its halves: there the next stage has landed
 // and this one has been read by all waves.
-template <int BM, int BN, int WM, int WN, int FMT, typename OutT>
-__global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a) {
+template <int BM, int BN, int WM, int WN, int NB, int PERCU, int FMT, typename OutT>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_tiles(
+    const Args a) {
   constexpr int kWaves = WM * WN;
   constexpr int kHalf = mx_half_bytes(FMT), kTile = 2 * kHalf;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-  // LDS: three stages of activations and scale words; of each half of the columns
-  // two pairs of weights
-  constexpr int kXBytes = BM / 32 * kTile, kXScale = kXBytes, kWScale = kXScale + BM * 4;
-  constexpr int kStage = kWScale + BN * 4, kPair = BN / 2 * 128, kWeights = 3 * kStage;
+  // LDS: NB stages of activations and scale words; of each half of the columns
+  // (NB + 1) / 2 pairs of weights
+  constexpr int kXRows = BM < 64 ? 64 : BM;  // scale words come by 64
+  constexpr int kXBytes = BM / 32 * kTile, kXScale = kXBytes, kWScale = kXScale + kXRows * 4;
+  constexpr int kStage = kWScale + BN * 4, kPair = BN / 2 * 128, kWeights = NB * kStage;
+  constexpr int kPairs = (NB + 1) / 2, kLds = kWeights + 2 * kPairs * kPair;
   // loads of 1 KiB (codes) and 256 bytes (scales) per stage, and per wave; a wave
   // without one repeats the last
-  constexpr int kXLoads = kXBytes / 1024, kWLoads = kPair / 1024, kSLoads = (BM + BN) / 64;
+  constexpr int kXLoads = kXBytes / 1024, kWLoads = kPair / 1024, kSLoads = (kXRows + BN) / 64;
   constexpr int kXPer = (kXLoads + kWaves - 1) / kWaves, kWPer = (kWLoads + kWaves - 1) / kWaves;
   constexpr int kSPer = (kSLoads + kWaves - 1) / kWaves, kLoads = kXPer + kSPer + kWPer;
-  static_assert(BM % 64 == 0 && BN % 64 == 0 && kWeights + 4 * kPair <= 160 * 1024, "tile");
-  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[kWeights + 4 * kPair];
+  static_assert(BM % 32 == 0 && BN % 64 == 0 && NB % 2 == 1 && NB >= 3, "tile");
+  static_assert(PERCU * kLds <= 160 * 1024 && (NB - 1) * kLoads + kWPer < 64, "tile");
+  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[kLds];
 
   const int tid = int(threadIdx.x), lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -107,8 +111,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
   const int nt = rest / high, mt = band * kBand + rest - nt * high;
   const int64_t m0 = int64_t(mt) * BM, n0 = int64_t(nt) * BN;
   const int stages = int(a.x.stages);
-  const int first = int(int64_t(stages) * split / a.splits);
-  const int count = int(int64_t(stages) * (split + 1) / a.splits) - first;
+  const int pairs = (stages + 1) / 2;  // (splits begin at whole pairs: whole lines)
+  const int first = pairs * split / a.splits * 2;
+  const int count = min(pairs * (split + 1) / a.splits * 2, stages) - first;
 
   // ---- loads of a stage ----
   const int mrows = int(min(int64_t(BM), a.x.rows32 - m0));   // a multiple of 32
@@ -145,12 +150,13 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
 #pragma unroll
   for (int i = 0; i < kSPer; ++i) {
     const int j = min(wave + i * kWaves, kSLoads - 1);
-    soff[i] = j < BM / 64 ? uint32_t(min(j * 64 + lane, mrows - 1) * 4)
-                          : uint32_t(min((j - BM / 64) * 64 + lane, nrows - 1) * 4);
+    soff[i] = j < kXRows / 64 ? uint32_t(min(j * 64 + lane, mrows - 1) * 4)
+                              : uint32_t(min((j - kXRows / 64) * 64 + lane, nrows - 1) * 4);
   }
-  // load k of this wave (constant) for stage t into stage buffer buf, and its offset
-  // one stage or pair on; the last weight load hands over to the other columns
-  auto issue = [&](auto K, int t, int buf) MX_INLINE {
+  // Load k of this wave (constant) for stage t into stage buffer buf and, the weights
+  // of the stage's half of the columns, into its pair buffer lpair; the offsets one
+  // stage or pair on, the weights' exchanged with the other half's.
+  auto issue = [&](auto K, int t, int buf, int lpair) MX_INLINE {
     const bool live = t < count;
     constexpr int k = decltype(K)::value;
     uint8_t* const s = s_mem + buf * kStage;
@@ -162,7 +168,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
     } else if constexpr (k < kXPer + kSPer) {
       constexpr int i = k - kXPer;
       const int j = min(wave + i * kWaves, kSLoads - 1);
-      const bool is_x = j < BM / 64;
+      const bool is_x = j < kXRows / 64;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           rsrc(is_x ? static_cast<const void*>(xsp) : wsp, live ? is_x ? xsbytes : wsbytes : 0),
           (lds_void*)(s + kXScale + j * 256), 4, int(soff[i]), 0, 0, 0);
@@ -170,9 +176,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
     } else {
       constexpr int i = k - kXPer - kSPer;
       const int j = min(wave + i * kWaves, kWLoads - 1);
-      const int pair = (t & 1) * 2 + ((t + (t & 1)) >> 1 & 1);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rsrc(wp, live ? wbytes : 0), (lds_void*)(s_mem + kWeights + pair * kPair + j * 1024), 16,
+          rsrc(wp, live ? wbytes : 0),
+          (lds_void*)(s_mem + kWeights + ((t & 1) * kPairs + lpair) * kPair + j * 1024), 16,
           int(woff[0][i]), 0, 0, 0);
       const uint32_t other = woff[1][i];
       woff[1][i] = woff[0][i] + 128;
@@ -197,7 +203,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
   // the first row tile, all column tiles, the other row tiles
   constexpr int kXReads = FMT == HIGGS_MX_FP6 ? 3 : 2;
   constexpr int kReads = TM * kXReads + TN * 2;
-  auto read = [&](auto K, Half& f, int t, int buf, int h) MX_INLINE {
+  auto read = [&](auto K, Half& f, int t, int buf, int pair0, int pair1, int h) MX_INLINE {
     constexpr int k = decltype(K)::value;
     const uint8_t* const s = s_mem + buf * kStage;
     if constexpr (k >= kXReads && k < kXReads + TN * 2) {
@@ -205,7 +211,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
       const int row = (wn * TN + n) * 32 + r32;
       if constexpr ((k - kXReads) % 2 == 0) {
         const int side = row / (BN / 2);  // (the same in all lanes)
-        const int pair = __builtin_amdgcn_readfirstlane(side * 2 + ((t + side) >> 1 & 1));
+        const int pair = __builtin_amdgcn_readfirstlane(side ? kPairs + pair1 : pair0);
         const int odd = __builtin_amdgcn_readfirstlane((t + side) & 1);
         const int unit = (4 * odd + 2 * h + hi) ^ (row & 7);
         const u32x4 u = *reinterpret_cast<const u32x4*>(
@@ -257,8 +263,11 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
   // [L0, L1) (spread over all: a wave that issues several at a time waits for the
   // address unit, and its products wait behind them). The order is kept as written.
   constexpr int kProducts = TM * TN;
-  auto half = [&](const Half& now, auto H, Half& next, int nt, int nbuf, int nh, auto L0, auto L1,
-                  int lt, int lbuf) MX_INLINE {
+  struct Place {
+    int stage, buf, pair0, pair1;  // pair0, pair1: the pair buffers of both column halves
+  };
+  auto half = [&](const Half& now, auto H, Half& next, const Place& np, int nh, auto L0, auto L1,
+                  int lt, int lbuf, int lpair) MX_INLINE {
     constexpr int kOver = kProducts >= 4 ? kProducts * 3 / 4 : kProducts;
     constexpr int l0 = decltype(L0)::value, nl = decltype(L1)::value - l0;
     for_each<kProducts>([&](auto I) MX_INLINE {
@@ -267,43 +276,55 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_product_tiles(const Args a
       constexpr int ra = kReads * (i < kOver ? i : kOver) / kOver;
       constexpr int rb = kReads * (i + 1 < kOver ? i + 1 : kOver) / kOver;
       for_each<rb - ra>([&](auto J) MX_INLINE {
-        read(std::integral_constant<int, ra + decltype(J)::value>{}, next, nt, nbuf, nh);
+        read(std::integral_constant<int, ra + decltype(J)::value>{}, next, np.stage, np.buf,
+             np.pair0, np.pair1, nh);
       });
       constexpr int la = l0 + nl * i / kProducts, lb = l0 + nl * (i + 1) / kProducts;
       for_each<lb - la>([&](auto J) MX_INLINE {
-        issue(std::integral_constant<int, la + decltype(J)::value>{}, lt, lbuf);
+        issue(std::integral_constant<int, la + decltype(J)::value>{}, lt, lbuf, lpair);
       });
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  // The loads for stage t + 3 go out from the meeting of stage t on, where their
+  // The loads for stage t + NB go out from the meeting of stage t on, where their
   // buffers are free: the first of them in its half 1, the others in half 0 of stage
-  // t + 1. So at the meeting of stage t the loads for stage t + 2 may be outstanding,
-  // those for t + 1 not.
+  // t + 1. So at the meeting of stage t the loads for the stages from t + 2 may be
+  // outstanding, those for t + 1 not.
   using L0 = std::integral_constant<int, 0>;
   using LH = std::integral_constant<int, (kLoads + 1) / 2>;
   using LN = std::integral_constant<int, kLoads>;
   for_each<kWPer>([&](auto K) MX_INLINE {  // (the second columns' pair that ends with stage 0)
-    issue(std::integral_constant<int, kXPer + kSPer + decltype(K)::value>{}, -1, 0);
+    issue(std::integral_constant<int, kXPer + kSPer + decltype(K)::value>{}, -1, 0, 0);
   });
-  for_each<kLoads>([&](auto K) MX_INLINE { issue(K, 0, 0); });
-  for_each<kLoads>([&](auto K) MX_INLINE { issue(K, 1, 1); });
-  for_each<LH::value>([&](auto K) MX_INLINE { issue(K, 2, 2); });
-  wait_vm<kLoads + LH::value>();
+  for_each<NB - 1>([&](auto T) MX_INLINE {
+    constexpr int t = decltype(T)::value;
+    for_each<kLoads>([&](auto K) MX_INLINE { issue(K, t, t, (t + 1) / 2); });
+  });
+  for_each<LH::value>([&](auto K) MX_INLINE { issue(K, NB - 1, NB - 1, NB / 2); });
+  wait_vm<(NB - 2) * kLoads + LH::value>();
   wait_lds_and_meet();
   Half f0, f1;
-  for_each<kReads>([&](auto K) MX_INLINE { read(K, f0, 0, 0, 0); });
-  int buf = 0, before = 2;
+  for_each<kReads>([&](auto K) MX_INLINE { read(K, f0, 0, 0, 0, 0, 0); });
+  // lpair: the pair buffer of the loads for stage t + NB - 1; pair0, pair1: those of
+  // stage t. A pair's buffer is taken up two stages later by the pair kPairs on.
+  Place at{0, 0, 0, 0};
+  int before = NB - 1, lpair = NB / 2;
+  auto wrap = [](int v, int n) MX_INLINE { return v == n ? 0 : v; };
   for (int t = 0; t < count; ++t) {
-    const int next = buf == 2 ? 0 : buf + 1;
+    const int odd = t & 1;
+    const Place next{t + 1, wrap(at.buf + 1, NB), wrap(at.pair0 + odd, kPairs),
+                     wrap(at.pair1 + 1 - odd, kPairs)};
     __builtin_amdgcn_sched_barrier(0);
-    half(f0, H0{}, f1, t, buf, 1, LH{}, LN{}, t + 2, before);
-    wait_vm<kLoads>();
+    half(f0, H0{}, f1, at, 1, LH{}, LN{}, t + NB - 1, before, lpair);
+    wait_vm<(NB - 2) * kLoads>();
     wait_lds_and_meet();
     __builtin_amdgcn_sched_barrier(0);
-    half(f1, H1{}, f0, t + 1, next, 0, L0{}, LH{}, t + 3, buf);
-    before = buf;
-    buf = next;
+    // (stage t + NB's columns' half is that of stage t + 1: its last pair has ended)
+    const int freed = odd ? at.pair0 : at.pair1;
+    half(f1, H1{}, f0, next, 0, L0{}, LH{}, t + NB, at.buf, freed);
+    before = at.buf;
+    lpair = freed;
+    at = next;
   }
   wait_vm<0>();
 
@@ -385,12 +406,53 @@ __global__ __launch_bounds__(256) void mx_scale_words(const uint8_t* __restrict_
   }
 }
 
+// Sums of the splits in their order, four outputs at a time.
+template <typename OutT>
+__global__ __launch_bounds__(256) void mx_sum_splits(const float* __restrict__ part, int splits,
+                                                     int64_t total, OutT* __restrict__ y) {
+  typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
+  if (i >= total) return;
+  const int n = int(min(total - i, int64_t(4)));
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (n == 4) {
+    for (int s = 0; s < splits; ++s) {
+      const f32x4_a4 u = *reinterpret_cast<const f32x4_a4*>(part + s * total + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] += u[j];
+    }
+  } else {
+    for (int s = 0; s < splits; ++s)
+      for (int j = 0; j < n; ++j) v[j] += part[s * total + i + j];
+  }
+  if constexpr (sizeof(OutT) == 4) {
+    if (n == 4)
+      *reinterpret_cast<float4*>(y + i) = make_float4(v[0], v[1], v[2], v[3]);
+    else
+      for (int j = 0; j < n; ++j) y[i + j] = v[j];
+  } else {
+    if (n == 4)
+      *reinterpret_cast<uint2*>(y + i) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+    else
+      for (int j = 0; j < n; ++j) y[i + j] = OutT(pack_bf16(v[j], 0.f));
+  }
+}
+
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
-// The workspace: activation codes and scales, weight scale words.
+// The block shapes.
+struct Shape {
+  int bm, bn, percu;
+};
+constexpr Shape kShapes[] = {{256, 256, 1}, {128, 128, 2}, {64, 128, 2}, {32, 128, 2}, {128, 256, 1}};
+constexpr int kNumShapes = int(sizeof(kShapes) / sizeof(kShapes[0]));
+
+// A call's shape, splits and workspace: activation codes and scales, weight scale
+// words, partial sums.
 struct Plan {
-  int64_t stages, rows32, x_bytes, xs_bytes, ws_bytes;
-  int64_t bytes() const { return x_bytes + xs_bytes + ws_bytes; }
+  int shape, splits;
+  int64_t stages, rows32, x_bytes, xs_bytes, ws_bytes, part_bytes;
+  int64_t bytes() const { return x_bytes + xs_bytes + ws_bytes + part_bytes; }
 };
 Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt) {
   Plan p;
@@ -399,17 +461,43 @@ Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt) {
   p.x_bytes = up256(p.rows32 / 32 * p.stages * 2 * mx_half_bytes(fmt));
   p.xs_bytes = up256(p.rows32 * p.stages * 4);
   p.ws_bytes = up256(out * p.stages * 4);
+  p.shape = 0;
+  p.splits = 1;
+  p.part_bytes = p.splits > 1 ? up256(p.splits * batch * out * 4) : 0;
   return p;
 }
 
-template <int BM, int BN, int WM, int WN, int FMT, typename OutT>
-hipError_t launch_tiles(Args a, hipStream_t stream) {
-  a.mtiles = int((a.batch + BM - 1) / BM);
-  a.ntiles = int((a.out + BN - 1) / BN);
-  a.splits = 1;
-  const auto kernel = mx_product_tiles<BM, BN, WM, WN, FMT, OutT>;
-  hipLaunchKernelGGL(kernel, dim3(unsigned(a.mtiles * a.ntiles * a.splits)), dim3(64 * WM * WN),
-                     0, stream, a);
+template <int BM, int BN, int WM, int WN, int NB, int PERCU, int FMT, typename OutT>
+hipError_t launch_tiles(const Args& a, hipStream_t stream) {
+  hipLaunchKernelGGL((mx_product_tiles<BM, BN, WM, WN, NB, PERCU, FMT, OutT>),
+                     dim3(unsigned(a.mtiles) * unsigned(a.ntiles) * unsigned(a.splits)),
+                     dim3(64 * WM * WN), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int FMT, typename OutT>
+hipError_t launch_shape(int shape, Args a, hipStream_t stream) {
+  a.mtiles = int((a.batch + kShapes[shape].bm - 1) / kShapes[shape].bm);
+  a.ntiles = int((a.out + kShapes[shape].bn - 1) / kShapes[shape].bn);
+  switch (shape) {
+    case 0: return launch_tiles<256, 256, 4, 2, 3, 1, FMT, OutT>(a, stream);
+    case 1: return launch_tiles<128, 128, 2, 2, 3, 2, FMT, OutT>(a, stream);
+    case 2: return launch_tiles<64, 128, 2, 2, 3, 2, FMT, OutT>(a, stream);
+    case 3: return launch_tiles<32, 128, 1, 4, 5, 2, FMT, OutT>(a, stream);
+    default: return launch_tiles<128, 256, 2, 4, 3, 1, FMT, OutT>(a, stream);
+  }
+}
+
+template <int FMT, typename OutT>
+hipError_t launch_product(const Plan& p, const Args& args, float* part, hipStream_t stream) {
+  Args a = args;
+  a.splits = p.splits;
+  if (p.splits > 1) a.y = part;
+  const hipError_t st = launch_shape<FMT, OutT>(p.shape, a, stream);
+  if (st != hipSuccess || p.splits == 1) return st;
+  const int64_t total = a.batch * a.out;
+  hipLaunchKernelGGL((mx_sum_splits<OutT>), dim3(unsigned((total + 1023) / 1024)), dim3(256), 0,
+                     stream, part, p.splits, total, static_cast<OutT*>(args.y));
   return hipGetLastError();
 }
 
@@ -426,11 +514,12 @@ hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, 
                              void* workspace, hipStream_t stream) {
   const Plan p = plan_of(batch, out, in, fmt);
   uint8_t* const w = static_cast<uint8_t*>(workspace);
+  uint32_t* const words = reinterpret_cast<uint32_t*>(w + p.x_bytes + p.xs_bytes);
+  float* const part = reinterpret_cast<float*>(w + p.x_bytes + p.xs_bytes + p.ws_bytes);
   Args a{};
   a.x = MxTiles{w, w + p.x_bytes, p.stages, p.rows32};
   hipError_t st = launch_mx_tiles(x, x_dtype, batch, in, fmt, g, seed, a.x, stream);
   if (st != hipSuccess) return st;
-  uint32_t* const words = reinterpret_cast<uint32_t*>(w + p.x_bytes + p.xs_bytes);
   a.wc = codes;
   a.ws = words;
   a.y = y;
@@ -438,17 +527,16 @@ hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, 
   a.out = out;
   a.blocks = int(mx_blocks(in));
   hipLaunchKernelGGL(mx_scale_words,
-                     dim3(unsigned((out + 63) / 64), unsigned(std::min<int64_t>((p.stages + 15) / 16, 64))),
+                     dim3(unsigned((out + 63) / 64),
+                          unsigned(std::min<int64_t>((p.stages + 15) / 16, 64))),
                      dim3(256), 0, stream, scales, out, a.blocks, int(p.stages), words);
   st = hipGetLastError();
   if (st != hipSuccess) return st;
   if (fmt == HIGGS_MX_FP4)
-    return y_dtype == HIGGS_F32
-               ? launch_tiles<256, 256, 4, 2, HIGGS_MX_FP4, float>(a, stream)
-               : launch_tiles<256, 256, 4, 2, HIGGS_MX_FP4, uint16_t>(a, stream);
-  return y_dtype == HIGGS_F32
-             ? launch_tiles<256, 256, 4, 2, HIGGS_MX_FP6, float>(a, stream)
-             : launch_tiles<256, 256, 4, 2, HIGGS_MX_FP6, uint16_t>(a, stream);
+    return y_dtype == HIGGS_F32 ? launch_product<HIGGS_MX_FP4, float>(p, a, part, stream)
+                                : launch_product<HIGGS_MX_FP4, uint16_t>(p, a, part, stream);
+  return y_dtype == HIGGS_F32 ? launch_product<HIGGS_MX_FP6, float>(p, a, part, stream)
+                              : launch_product<HIGGS_MX_FP6, uint16_t>(p, a, part, stream);
 }
 
 }  // namespace higgs
