@@ -33,6 +33,7 @@ SOURCES = {
     "qgemm_wide.hip": [],
     "scratch.hip": [],
     "mx_quant.hip": [],
+    "mx_decode.hip": [],
     "mx_product.hip": [],
 }
 

@@ -55,6 +55,13 @@ hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int
 hipError_t launch_mx_layer_error(const void* w, higgs_dtype dtype, int64_t out, int64_t in,
                                  const uint8_t* codes, const uint8_t* scales, int g, uint64_t seed,
                                  double* row_err, double* t2, hipStream_t stream);
+// Few rows (mx_decode.hip): activations from `tiles`, or, where mx_decode_fuses,
+// raw ones converted on the way (`tiles` is not read). batch <= 32.
+bool mx_decode_fuses(int64_t batch, int64_t in, int g);
+hipError_t launch_mx_decode(const void* x, higgs_dtype x_dtype, int64_t batch, int fmt,
+                            const MxTiles& tiles, const uint8_t* codes, const uint8_t* scales,
+                            int g, uint64_t seed, int64_t out, int64_t in, void* y,
+                            higgs_dtype y_dtype, hipStream_t stream);
 int64_t mx_qmatmul_workspace_bytes(int64_t batch, int64_t out, int64_t in, int fmt, int g);
 hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, int fmt,
                              const uint8_t* codes, const uint8_t* scales, int g, uint64_t seed,

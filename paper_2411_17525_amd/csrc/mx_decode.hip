@@ -1,0 +1,332 @@
+// The microscaled product for few activation rows: a stream of the weights.
+//
+// A block takes tiles of 16 outputs, one after another; its waves share K in
+// chunks of 512 (256 bytes of a weight row). A wave's chunk of a tile, 4 KiB, goes
+// from memory into the wave's own LDS slots, RING chunks ahead and with whole lines
+// of each row, and from there into the 16x16x128 scaled matrix instruction, whose
+// other operand is up to 16 activation rows; 32 with two of them. The waves' sums
+// of a tile meet in LDS and are added in the waves' order.
+//
+// The activations come from the product's workspace (MxTiles), or, for calls that
+// convert little (FUSED), each block rotates and quantizes them itself while its
+// first weights are on their way, into LDS: one launch instead of two.
+
+#include <algorithm>
+
+#include "mx_device.h"
+
+namespace higgs {
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) void lds_void;
+
+constexpr int kMaxWaves = 8;
+// Values that a block converts itself: above that the conversion takes longer than
+// the launch that it saves.
+constexpr int kFusedValues = 16384;
+
+struct Args {
+  const void* x;  // FUSED: raw activations
+  MxTiles t;      // otherwise
+  const uint8_t* wc;
+  const uint8_t* ws;
+  void* y;
+  int64_t out;
+  int batch, in, blocks, stages, chunks, tiles;
+  int x_bf16, y_bf16;
+  double root;
+  MxSigns signs;
+};
+
+__device__ inline __amdgpu_buffer_rsrc_t rsrc(const void* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, int(bytes), 0x00020000);
+}
+
+// The wave's LDS reads and writes are done, then all waves meet (loads to LDS for
+// later chunks stay in flight).
+__device__ inline void wait_lds_and_meet() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// G: FUSED with groups of G (0: no rotation); -1: activations from t. NT: tiles of
+// 16 activation rows.
+template <int FMT, int G, int NT>
+__global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
+  constexpr bool kFused = G >= 0;
+  constexpr int RING = kFused ? 2 : 3;
+  constexpr int kSlot = 4096, kUnit2 = FMT == HIGGS_MX_FP6 ? 8 : 0;
+  // LDS: the waves' slots; two tiles' partial sums; FUSED: the activations (16- and
+  // 8-byte parts, scale words) and the rotation's scratch
+  constexpr int kRing = kMaxWaves * RING * kSlot, kPart = kMaxWaves * NT * 16 * 16 * 4;
+  constexpr int kXBlocks = kFused ? kFusedValues / 32 + 16 * 16 : 0;  // (whole stages per row)
+  constexpr int kX = kRing + 2 * kPart, kXTail = kX + kXBlocks * 16;
+  constexpr int kXScale = kXTail + kXBlocks * kUnit2, kScratch = kXScale + kXBlocks;
+  constexpr int kLds = kScratch + (G > 0 ? kMaxWaves * kMxWaveLds * 4 : 0);
+  static_assert(kLds <= 160 * 1024, "LDS");
+  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[kLds];
+
+  const int tid = int(threadIdx.x), lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int waves = int(blockDim.x) >> 6;
+  const int r16 = lane & 15, q = lane >> 4;
+
+  // ---- weights: chunk c of tile t into the wave's slot ----
+  const __amdgpu_buffer_rsrc_t wrs = rsrc(a.wc, uint32_t(a.out * a.blocks * 16));
+  uint8_t* const ring = s_mem + wave * RING * kSlot;
+  const int mine = (a.chunks - wave + waves - 1) / waves;  // chunks wave, wave + waves, ..
+  // 4 rows of 256 bytes per load; a row's 16 blocks are permuted so that eight rows of
+  // one block lie in distinct banks
+  auto issue = [&](int tile, int chunk, int slot) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = 4 * j + q, unit = r16 ^ (row & 7);
+      const uint32_t at = uint32_t(min(int64_t(tile) * 16 + row, a.out - 1)) * uint32_t(a.blocks * 16) +
+                          uint32_t(chunk * 256 + unit * 16);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(wrs, (lds_void*)(ring + slot * kSlot + j * 1024), 16,
+                                               int(at), 0, 0, 0);
+    }
+  };
+  // ---- the scale bytes of the lane's row: a word per stage of the chunk ----
+  auto load_scales = [&](int tile, int chunk, uint32_t (&s)[4]) {
+    const uint8_t* const p =
+        a.ws + min(int64_t(tile) * 16 + r16, a.out - 1) * a.blocks + chunk * 16;
+    const int left = a.blocks - chunk * 16;
+    if (left >= 16) {
+      typedef uint32_t u32x4_a1 __attribute__((ext_vector_type(4), aligned(1)));
+      const u32x4_a1 u = *reinterpret_cast<const u32x4_a1*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = u[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[i] = 0;
+        for (int j = 0; j < 4; ++j)
+          if (4 * i + j < left) s[i] |= uint32_t(p[4 * i + j]) << (8 * j);
+      }
+    }
+  };
+
+  // items of the wave: its chunks of the block's tiles
+  int it = int(blockIdx.x), ik = 0;  // tile and chunk number of the next item to request
+  auto request = [&](int slot) {
+    if (it < a.tiles) issue(it, wave + ik * waves, slot);
+    if (++ik == mine) {
+      ik = 0;
+      it += int(gridDim.x);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < RING - 1; ++i) request(i);
+
+  // ---- FUSED: the activations into LDS; block kb of row b is unit kb * batch + b ----
+  const int batch = a.batch;
+  if constexpr (kFused) {
+    auto put = [&](int b, int half, const uint32_t* c) {
+      uint8_t* const head = s_mem + kX + ((half >> 1) * batch + b) * 16;
+      if constexpr (FMT == HIGGS_MX_FP4) {
+        *reinterpret_cast<u32x2*>(head + (half & 1) * 8) = u32x2{c[0], c[1]};
+      } else {
+        uint32_t* const h = reinterpret_cast<uint32_t*>(head);
+        uint32_t* const t = reinterpret_cast<uint32_t*>(s_mem + kXTail + ((half >> 1) * batch + b) * 8);
+        if ((half & 1) == 0) {
+          h[0] = c[0];
+          h[1] = c[1];
+          h[2] = c[2];
+        } else {
+          h[3] = c[0];
+          t[0] = c[1];
+          t[1] = c[2];
+        }
+      }
+    };
+    auto put_scale = [&](int b, int kb, uint32_t byte) {
+      s_mem[kXScale + ((kb >> 2) * batch + b) * 4 + (kb & 3)] = uint8_t(byte);
+    };
+    auto load = [&](int b, int k, float (&x)[16]) {
+      const int left = a.in - k, n = left < 0 ? 0 : left > 16 ? 16 : left;
+      const int64_t at = int64_t(b) * a.in + (left > 0 ? k : 0);
+      if (a.x_bf16)
+        load16_upto(static_cast<const uint16_t*>(a.x) + at, n, x);
+      else
+        load16_upto(static_cast<const float*>(a.x) + at, n, x);
+    };
+    if constexpr (G > 0) {
+      uint32_t* const lds = reinterpret_cast<uint32_t*>(s_mem + kScratch) + wave * kMxWaveLds;
+      const uint32_t neg = lane_signs<G>(a.signs, lane);
+      const int segs = (a.in + 1023) / 1024;  // of a row; the last may end early
+      for (int i = wave; i < batch * segs; i += waves) {
+        const int b = i / segs, seg = i - b * segs;
+        float x[16];
+        load(b, 1024 * seg + 16 * lane, x);
+        uint32_t c[kWords16<FMT>], byte;
+        int block;
+        mx_rotate_segment<G, FMT>(x, neg, a.root, lds, lane, c, &byte, &block);
+        // (up to the end of the row's last stage: zeros behind its values)
+        const int half = 64 * seg + lane;
+        if (half < 8 * a.stages) put(b, half, c);
+        const int kb = 32 * seg + block;
+        if ((lane & 15) < 8 && kb < 4 * a.stages) put_scale(b, kb, byte);
+      }
+    } else {
+      const int units = 8 * a.stages;
+      for (int u = tid; u < batch * units; u += 64 * waves) {
+        const int b = u / units, half = u - b * units;
+        float x[16];
+        load(b, 16 * half, x);
+        uint32_t c[kWords16<FMT>];
+        const uint32_t byte = mx_plain_halves<FMT>(x, c);
+        put(b, half, c);
+        if ((half & 1) == 0) put_scale(b, half >> 1, byte);
+      }
+    }
+    wait_lds_and_meet();
+  }
+
+  // ---- activations of stage t: block q of row r16 (+ 16) ----
+  auto load_x = [&](int t, int n, i32x8& x, uint32_t& s) {
+    u32x4 u;
+    u32x2 v = {0, 0};
+    if constexpr (kFused) {
+      const int at = (4 * t + q) * batch + min(r16, batch - 1);
+      u = *reinterpret_cast<const u32x4*>(s_mem + kX + at * 16);
+      if constexpr (FMT == HIGGS_MX_FP6) v = *reinterpret_cast<const u32x2*>(s_mem + kXTail + at * 8);
+      s = *reinterpret_cast<const uint32_t*>(s_mem + kXScale + (t * batch + min(r16, batch - 1)) * 4);
+    } else {
+      const uint8_t* const p = a.t.codes + (t * 2 + (q >> 1)) * mx_half_bytes(FMT);
+      const int unit = (q & 1) * 32 + n * 16 + r16;
+      u = *reinterpret_cast<const u32x4*>(p + unit * 16);
+      if constexpr (FMT == HIGGS_MX_FP6) v = *reinterpret_cast<const u32x2*>(p + 1024 + unit * 8);
+      s = *reinterpret_cast<const uint32_t*>(a.t.scales + (t * 32 + n * 16 + r16) * 4);
+    }
+    x = i32x8{int(u[0]), int(u[1]), int(u[2]), int(u[3]), int(v[0]), int(v[1]), 0, 0};
+  };
+
+  // ---- the stream ----
+  int slot = 0, turn = 0;
+  for (int tile = int(blockIdx.x); tile < a.tiles; tile += int(gridDim.x), turn ^= 1) {
+    f32x4 acc[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < mine; ++k) {
+      const int chunk = wave + k * waves;
+      // behind this item's weights: its scales and activations, so that these have
+      // arrived (loads arrive in order) where the weights have
+      uint32_t ws[4];
+      load_scales(tile, chunk, ws);
+      i32x8 x[4][NT];
+      uint32_t xs[4][NT];
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) load_x(min(4 * chunk + s, a.stages - 1), n, x[s][n], xs[s][n]);
+      __builtin_amdgcn_sched_barrier(0);
+      request(slot == 0 ? RING - 1 : slot - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("" ::"v"(ws[0]), "v"(ws[1]), "v"(ws[2]), "v"(ws[3]) : "memory");
+      const uint8_t* const w0 = ring + slot * kSlot + r16 * 256;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const u32x4 u = *reinterpret_cast<const u32x4*>(w0 + ((4 * s + q) ^ (r16 & 7)) * 16);
+        const i32x8 w = {int(u[0]), int(u[1]), int(u[2]), int(u[3]), 0, 0, 0, 0};
+        if (4 * chunk + s < a.stages) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            acc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                x[s][n], w, acc[n], FMT == HIGGS_MX_FP4 ? 4 : 2, 4, 0, int(xs[s][n] >> (8 * q)), 0,
+                int(ws[s] >> (8 * q)));
+        }
+      }
+      // (the slot's reads are done before it is requested again: their data has been
+      // used above)
+      slot = slot == RING - 1 ? 0 : slot + 1;
+    }
+    // partial sums: rows 4 q + i of column r16
+    float* const part = reinterpret_cast<float*>(s_mem + kRing + turn * kPart);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int b = n * 16 + 4 * q + i;
+        if (b < batch) part[(wave * NT * 16 + b) * 16 + r16] = acc[n][i];
+      }
+    wait_lds_and_meet();
+    for (int i = tid; i < batch * 16; i += 64 * waves) {
+      float t = 0.f;
+      for (int w = 0; w < waves; ++w) t += part[w * NT * 256 + i];
+      const int64_t o = int64_t(tile) * 16 + (i & 15);
+      if (o < a.out) {
+        const int64_t at = (i >> 4) * a.out + o;
+        if (a.y_bf16)
+          static_cast<uint16_t*>(a.y)[at] = uint16_t(pack_bf16(t, 0.f));
+        else
+          static_cast<float*>(a.y)[at] = t;
+      }
+    }
+  }
+}
+
+template <int FMT, int G, int NT>
+hipError_t launch(const Args& a, int waves, hipStream_t stream) {
+  // one block per compute unit, or fewer
+  hipLaunchKernelGGL((mx_decode<FMT, G, NT>), dim3(unsigned(std::min(a.tiles, 256))),
+                     dim3(unsigned(64 * waves)), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int FMT>
+hipError_t launch_fmt(const Args& a, int waves, bool fused, int g, hipStream_t stream) {
+  if (!fused)
+    return a.batch <= 16 ? launch<FMT, -1, 1>(a, waves, stream)
+                         : launch<FMT, -1, 2>(a, waves, stream);
+  switch (g) {
+    case 0: return launch<FMT, 0, 1>(a, waves, stream);
+    case 64: return launch<FMT, 64, 1>(a, waves, stream);
+    case 128: return launch<FMT, 128, 1>(a, waves, stream);
+    case 256: return launch<FMT, 256, 1>(a, waves, stream);
+    case 512: return launch<FMT, 512, 1>(a, waves, stream);
+    default: return launch<FMT, 1024, 1>(a, waves, stream);
+  }
+}
+
+}  // namespace
+
+bool mx_decode_fuses(int64_t batch, int64_t in, int g) {
+  return batch <= 16 && g <= 1024 && batch * in <= kFusedValues;
+}
+
+hipError_t launch_mx_decode(const void* x, higgs_dtype x_dtype, int64_t batch, int fmt,
+                            const MxTiles& tiles, const uint8_t* codes, const uint8_t* scales,
+                            int g, uint64_t seed, int64_t out, int64_t in, void* y,
+                            higgs_dtype y_dtype, hipStream_t stream) {
+  const bool fused = mx_decode_fuses(batch, in, g);
+  Args a;
+  a.x = x;
+  a.t = tiles;
+  a.wc = codes;
+  a.ws = scales;
+  a.y = y;
+  a.out = out;
+  a.batch = int(batch);
+  a.in = int(in);
+  a.blocks = int(mx_blocks(in));
+  a.stages = int((in + 127) / 128);
+  a.chunks = (a.stages + 3) / 4;
+  a.tiles = int((out + 15) / 16);
+  a.x_bf16 = x_dtype == HIGGS_BF16;
+  a.y_bf16 = y_dtype == HIGGS_BF16;
+  a.root = 0.0;
+  if (fused && g > 0) {
+    a.root = 1.0 / std::sqrt(double(g));
+    mx_signs(seed, g, &a.signs);
+  }
+  // as few waves as take equal shares of the chunks in as many turns as eight would
+  const int turns = (a.chunks + kMaxWaves - 1) / kMaxWaves;
+  const int waves = (a.chunks + turns - 1) / turns;
+  return fmt == HIGGS_MX_FP4 ? launch_fmt<HIGGS_MX_FP4>(a, waves, fused, g, stream)
+                             : launch_fmt<HIGGS_MX_FP6>(a, waves, fused, g, stream);
+}
+
+}  // namespace higgs

@@ -447,22 +447,28 @@ struct Shape {
 constexpr Shape kShapes[] = {{256, 256, 1}, {128, 128, 2}, {64, 128, 2}, {32, 128, 2}, {128, 256, 1}};
 constexpr int kNumShapes = int(sizeof(kShapes) / sizeof(kShapes[0]));
 
+constexpr int64_t kDecodeRows = 32;  // up to here the weights are streamed
+
 // A call's shape, splits and workspace: activation codes and scales, weight scale
 // words, partial sums.
 struct Plan {
-  int shape, splits;
+  int shape, splits;  // shape -1: mx_decode
   int64_t stages, rows32, x_bytes, xs_bytes, ws_bytes, part_bytes;
   int64_t bytes() const { return x_bytes + xs_bytes + ws_bytes + part_bytes; }
 };
-Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt) {
-  Plan p;
+Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt, int g) {
+  Plan p{};
+  p.shape = batch <= kDecodeRows ? -1 : 0;
+  p.splits = 1;
   p.stages = (in + 127) / 128;
   p.rows32 = (batch + 31) / 32 * 32;
   p.x_bytes = up256(p.rows32 / 32 * p.stages * 2 * mx_half_bytes(fmt));
   p.xs_bytes = up256(p.rows32 * p.stages * 4);
+  if (p.shape < 0) {
+    if (mx_decode_fuses(batch, in, g)) p.x_bytes = p.xs_bytes = 0;
+    return p;
+  }
   p.ws_bytes = up256(out * p.stages * 4);
-  p.shape = 0;
-  p.splits = 1;
   p.part_bytes = p.splits > 1 ? up256(p.splits * batch * out * 4) : 0;
   return p;
 }
@@ -504,22 +510,25 @@ hipError_t launch_product(const Plan& p, const Args& args, float* part, hipStrea
 }  // namespace
 
 int64_t mx_qmatmul_workspace_bytes(int64_t batch, int64_t out, int64_t in, int fmt, int g) {
-  (void)g;
-  return plan_of(batch, out, in, fmt).bytes();
+  return plan_of(batch, out, in, fmt, g).bytes();
 }
 
 hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, int fmt,
                              const uint8_t* codes, const uint8_t* scales, int g, uint64_t seed,
                              int64_t out, int64_t in, void* y, higgs_dtype y_dtype,
                              void* workspace, hipStream_t stream) {
-  const Plan p = plan_of(batch, out, in, fmt);
+  const Plan p = plan_of(batch, out, in, fmt, g);
   uint8_t* const w = static_cast<uint8_t*>(workspace);
   uint32_t* const words = reinterpret_cast<uint32_t*>(w + p.x_bytes + p.xs_bytes);
   float* const part = reinterpret_cast<float*>(w + p.x_bytes + p.xs_bytes + p.ws_bytes);
   Args a{};
   a.x = MxTiles{w, w + p.x_bytes, p.stages, p.rows32};
-  hipError_t st = launch_mx_tiles(x, x_dtype, batch, in, fmt, g, seed, a.x, stream);
+  hipError_t st = hipSuccess;
+  if (p.x_bytes > 0) st = launch_mx_tiles(x, x_dtype, batch, in, fmt, g, seed, a.x, stream);
   if (st != hipSuccess) return st;
+  if (p.shape < 0)
+    return launch_mx_decode(x, x_dtype, batch, fmt, a.x, codes, scales, g, seed, out, in, y, y_dtype,
+                            stream);
   a.wc = codes;
   a.ws = words;
   a.y = y;

@@ -18,8 +18,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "mx.h"
-#include "wave_fwht.h"
+#include "mx_device.h"
 
 namespace higgs {
 
@@ -49,103 +48,6 @@ void mx_signs(uint64_t seed, int g, MxSigns* s) {
 namespace {
 
 constexpr int kWaves = 4;
-// LDS dwords per wave: fwht_rows's scratch, or 1024 fp32 values
-constexpr int kWaveLds = kFwhtRows > 1024 ? kFwhtRows : 1024;
-
-// 16 consecutive values from p (aligned to the type only).
-template <typename InT>
-__device__ inline void load16(const InT* p, float (&v)[16]) {
-  if constexpr (sizeof(InT) == 2) {
-    typedef uint16_t u16x8 __attribute__((ext_vector_type(8), aligned(2)));
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const u16x8 u = *reinterpret_cast<const u16x8*>(p + 8 * h);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[8 * h + i] = bf16_to_f32(u[i]);
-    }
-  } else {
-    typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const f32x4 u = *reinterpret_cast<const f32x4*>(p + 4 * h);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[4 * h + i] = u[i];
-    }
-  }
-}
-
-template <typename InT>
-__device__ inline float load1(const InT* p) {
-  if constexpr (sizeof(InT) == 2) {
-    return bf16_to_f32(*p);
-  } else {
-    return *p;
-  }
-}
-
-// n values (0 .. 16) from p, zeros behind them.
-template <typename InT>
-__device__ inline void load16_upto(const InT* p, int n, float (&v)[16]) {
-  if (n >= 16) {
-    load16(p, v);
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = i < n ? load1(p + i) : 0.f;
-}
-
-template <typename OutT>
-__device__ inline void store16(OutT* p, const float (&v)[16]) {
-  if constexpr (sizeof(OutT) == 2) {
-    typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      u32x4_a2 u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        u[i] = pack_bf16(v[8 * h + 2 * i], v[8 * h + 2 * i + 1]);
-      *reinterpret_cast<u32x4_a2*>(p + 8 * h) = u;
-    }
-  } else {
-    typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
-#pragma unroll
-    for (int h = 0; h < 4; ++h)
-      *reinterpret_cast<f32x4*>(p + 4 * h) =
-          f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-  }
-}
-
-template <typename OutT>
-__device__ inline void store16_upto(OutT* p, int n, const float (&v)[16]) {
-  if (n >= 16) {
-    store16(p, v);
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (i < n) {
-      if constexpr (sizeof(OutT) == 2) {
-        p[i] = OutT(pack_bf16(v[i], 0.f));
-      } else {
-        p[i] = v[i];
-      }
-    }
-}
-
-// Codes of 16 values: 2 (E2M1) or 3 (E2M3) words.
-template <int FMT>
-constexpr int kWords16 = FMT == HIGGS_MX_FP4 ? 2 : 3;
-
-template <int FMT>
-__device__ inline void store_codes16(uint8_t* p, const uint32_t* c) {
-#pragma unroll
-  for (int i = 0; i < kWords16<FMT>; ++i) reinterpret_cast<uint32_t*>(p)[i] = c[i];
-}
-template <int FMT>
-__device__ inline void load_codes16(const uint8_t* p, uint32_t* c) {
-#pragma unroll
-  for (int i = 0; i < kWords16<FMT>; ++i) c[i] = reinterpret_cast<const uint32_t*>(p)[i];
-}
 
 // Where a quantizer's kernel puts half-block u of the matrix (16 codes) and block
 // u's scale byte, u counted along the rows: the caller's arrays, row after row.
@@ -206,90 +108,12 @@ struct TileSink {
   }
 };
 
-// The scale byte of a block from the largest fp32 or fp64 exponent field of its
-// values (255: NaN or infinity).
-__device__ inline uint32_t scale_byte_f32(uint32_t field) {
-  if (field == 255) return 255;
-  return field < uint32_t(kMxTop) ? 0 : field - kMxTop;
-}
-__device__ inline uint32_t scale_byte_f64(uint32_t field) {
-  if (field >= 1023 + 128) return 255;
-  const int b = int(field) - 1023 + 127 - kMxTop;
-  return uint32_t(b < 0 ? 0 : b);
-}
-__device__ inline uint32_t field_f64(double v) {
-  return uint32_t(__builtin_bit_cast(uint64_t, v) >> 52) & 0x7ff;
-}
-// 2^-E of a scale byte, as a double; 0 for the NaN byte (every code is 0 then).
-__device__ inline double inverse_scale(uint32_t byte) {
-  return byte == 255 ? 0.0
-                     : __builtin_bit_cast(double, uint64_t(1023 + 127 - byte) << 52);
-}
-__device__ inline float odd_scaled(double v, uint32_t byte) {
-  return byte == 255 ? 0.f : mx_odd_f32(v * inverse_scale(byte));
-}
-
-// The butterflies' sum times 1 / sqrt(g); a zero gets the sign + (which one the
-// sum leaves depends on its order).
-__device__ inline double normalised(double v, double root) {
-  return __builtin_fma(v, root, 0.0);
-}
-
-// Place of element n of a segment of 1024 in LDS: runs of 16 permuted so that
-// the four rows of lanes hit distinct banks.
-__device__ inline int lds_place(int n) { return n ^ ((((n >> 6) ^ (n >> 8)) & 3) << 4); }
-
-// Moves 16 fp32 values per lane from fwht_rows's places to 16 consecutive ones
-// per lane through the wave's LDS.
-template <int G>
-__device__ inline void rows_to_lanes(float (&v)[16], float* lds, int lane) {
-  wave_lds_sync();
-#pragma unroll
-  for (int r = 0; r < 16; ++r) lds[lds_place(fwht_rows_lane<G>(lane) + fwht_rows_reg<G>(r))] = v[r];
-  wave_lds_sync();
-  typedef float f32x4 __attribute__((ext_vector_type(4)));
-  const f32x4* p = reinterpret_cast<const f32x4*>(lds + lds_place(16 * lane));
-#pragma unroll
-  for (int h = 0; h < 4; ++h) {
-    const f32x4 u = p[h];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[4 * h + i] = u[i];
-  }
-  wave_lds_sync();
-}
-// And back.
-template <int G>
-__device__ inline void lanes_to_rows(float (&v)[16], float* lds, int lane) {
-  wave_lds_sync();
-  typedef float f32x4 __attribute__((ext_vector_type(4)));
-  f32x4* p = reinterpret_cast<f32x4*>(lds + lds_place(16 * lane));
-#pragma unroll
-  for (int h = 0; h < 4; ++h) p[h] = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-  wave_lds_sync();
-#pragma unroll
-  for (int r = 0; r < 16; ++r) v[r] = lds[lds_place(fwht_rows_lane<G>(lane) + fwht_rows_reg<G>(r))];
-  wave_lds_sync();
-}
-
-// This lane's 16 sign bits for elements 16 lane .. of a segment of 1024.
-template <int G>
-__device__ inline uint32_t lane_signs(const MxSigns& s, int lane) {
-  const int j = (16 * lane) & (G - 1);
-  return s.w[j >> 5] >> (j & 16);
-}
-
-template <int G>
-__device__ inline void signed_f64(const float (&x)[16], uint32_t neg, double (&v)[16]) {
-#pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = double((neg >> i) & 1 ? -x[i] : x[i]);
-}
-
 // ---- quantization ----
 
 template <int G, int FMT, typename InT, typename Sink>
 __global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht(
     const InT* __restrict__ w, int64_t total, const MxSigns signs, double root, const Sink sink) {
-  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kWaveLds];
+  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
   uint32_t* const lds = s_lds[wave];
   const uint32_t neg = lane_signs<G>(signs, lane);
@@ -304,38 +128,12 @@ __global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht(
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = 0.f;
     }
-    double v[16];
-    signed_f64<G>(x, neg, v);
-    fwht_rows<G>(v, lds, lane);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] = normalised(v[r], root);
-    // block b = r / 2: registers 2b and 2b + 1 of the row's 16 lanes
-    uint32_t byte[8];
-#pragma unroll
-    for (int b = 0; b < 8; ++b) {
-      uint32_t f = max(field_f64(v[2 * b]), field_f64(v[2 * b + 1]));
-      f = max(f, lane_xor_small<1>(f));
-      f = max(f, lane_xor_small<2>(f));
-      f = max(f, lane_xor_small<4>(f));
-      f = max(f, lane_xor_small<8>(f));
-      byte[b] = scale_byte_f64(f);
-    }
-    uint32_t mine = byte[0];
-#pragma unroll
-    for (int b = 1; b < 8; ++b) mine = (lane & 7) == b ? byte[b] : mine;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = odd_scaled(v[r], byte[r / 2]);
-    rows_to_lanes<G>(x, reinterpret_cast<float*>(lds), lane);
-    uint32_t c[kWords16<FMT>];
-    mx_encode16<FMT>(x, c);
+    uint32_t c[kWords16<FMT>], byte;
+    int block;
+    mx_rotate_segment<G, FMT>(x, neg, root, lds, lane, c, &byte, &block);
     if (live) sink.template put<FMT>(at / 16, c);
-    if ((lane & 15) < 8) {
-      int e = fwht_rows_lane<G>(lane & ~15);
-#pragma unroll
-      for (int b = 0; b < 8; ++b) e |= (lane & 7) == b ? fwht_rows_reg<G>(2 * b) : 0;
-      const int64_t first = 1024 * seg + e;
-      if (first < total) sink.put_scale(first / 32, mine);
-    }
+    const int64_t mine = 32 * seg + block;
+    if ((lane & 15) < 8 && 32 * mine < total) sink.put_scale(mine, byte);
   }
 }
 
@@ -394,16 +192,8 @@ __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__
     const int64_t left = in - k;
     float x[16];
     load16_upto(w + row * in + (left > 0 ? k : 0), int(left < 0 ? 0 : left > 16 ? 16 : left), x);
-    uint32_t f = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) f = max(f, __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffffu);
-    f = max(f, lane_xor_small<1>(f));
-    const uint32_t byte = scale_byte_f32(f >> 23);
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      x[i] = byte == 255 ? 0.f : __builtin_ldexpf(x[i], 127 - int(byte));
     uint32_t c[kWords16<FMT>];
-    mx_encode16<FMT>(x, c);
+    const uint32_t byte = mx_plain_halves<FMT>(x, c);
     if constexpr (std::is_same_v<Sink, TileSink>) {
       sink.template put_at<FMT>(uint32_t(row), uint32_t(u - row * units), c);
       if ((u & 1) == 0) sink.put_scale_at(uint32_t(row), uint32_t(u - row * units) >> 1, byte);
@@ -420,7 +210,7 @@ template <int G, int FMT, typename OutT>
 __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht(
     const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t total,
     const MxSigns signs, double root, OutT* __restrict__ w) {
-  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kWaveLds];
+  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
   uint32_t* const lds = s_lds[wave];
   const uint32_t neg = lane_signs<G>(signs, lane);
@@ -530,7 +320,7 @@ __global__ __launch_bounds__(64 * kWaves) void mx_error_rht(
     const InT* __restrict__ w, int64_t in, const MxSigns signs, double root,
     const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
     double* __restrict__ row_err) {
-  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kWaveLds];
+  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
   uint32_t* const lds = s_lds[wave];
   const uint32_t neg = lane_signs<G>(signs, lane);
