@@ -56,15 +56,16 @@ __device__ inline void wait_lds_and_meet() {
 template <int FMT, int G, int NT>
 __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
   constexpr bool kFused = G >= 0;
-  constexpr int RING = kFused ? 2 : 3;
+  constexpr int kRingSlots = 2;
   constexpr int kSlot = 4096, kUnit2 = FMT == HIGGS_MX_FP6 ? 8 : 0;
-  // LDS: the waves' slots; two tiles' partial sums; FUSED: the activations (16- and
-  // 8-byte parts, scale words) and the rotation's scratch
-  constexpr int kRing = kMaxWaves * RING * kSlot, kPart = kMaxWaves * NT * 16 * 16 * 4;
+  // LDS: the waves' slots, the last of them the rotation's scratch first; two tiles'
+  // partial sums; FUSED: the activations (16- and 8-byte parts, scale words)
+  constexpr int kWaveRing =
+      (kRingSlots - 1) * kSlot + (G > 0 ? std::max(kSlot, kMxWaveLds * 4) : kSlot);
+  constexpr int kRing = kMaxWaves * kWaveRing, kPart = kMaxWaves * NT * 16 * 16 * 4;
   constexpr int kXBlocks = kFused ? kFusedValues / 32 + 16 * 16 : 0;  // (whole stages per row)
   constexpr int kX = kRing + 2 * kPart, kXTail = kX + kXBlocks * 16;
-  constexpr int kXScale = kXTail + kXBlocks * kUnit2, kScratch = kXScale + kXBlocks;
-  constexpr int kLds = kScratch + (G > 0 ? kMaxWaves * kMxWaveLds * 4 : 0);
+  constexpr int kXScale = kXTail + kXBlocks * kUnit2, kLds = kXScale + kXBlocks;
   static_assert(kLds <= 160 * 1024, "LDS");
   __shared__ __attribute__((aligned(1024))) uint8_t s_mem[kLds];
 
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
 
   // ---- weights: chunk c of tile t into the wave's slot ----
   const __amdgpu_buffer_rsrc_t wrs = rsrc(a.wc, uint32_t(a.out * a.blocks * 16));
-  uint8_t* const ring = s_mem + wave * RING * kSlot;
+  uint8_t* const ring = s_mem + wave * kWaveRing;
   const int mine = (a.chunks - wave + waves - 1) / waves;  // chunks wave, wave + waves, ..
   // 4 rows of 256 bytes per load; a row's 16 blocks are permuted so that eight rows of
   // one block lie in distinct banks
@@ -109,17 +110,31 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
     }
   };
 
-  // items of the wave: its chunks of the block's tiles
-  int it = int(blockIdx.x), ik = 0;  // tile and chunk number of the next item to request
-  auto request = [&](int slot) {
-    if (it < a.tiles) issue(it, wave + ik * waves, slot);
-    if (++ik == mine) {
-      ik = 0;
-      it += int(gridDim.x);
+  // Items of the wave: its chunks of the block's tiles. An item's weights are requested
+  // before its scales: loads arrive in order, so that where these have arrived the
+  // weights have.
+  struct Next {
+    int tile, k;
+  };
+  auto advance = [&](Next& n) {
+    if (++n.k == mine) {
+      n.k = 0;
+      n.tile += int(gridDim.x);
     }
   };
-#pragma unroll
-  for (int i = 0; i < RING - 1; ++i) request(i);
+  struct Item {
+    uint32_t ws[4], xs[4][NT];
+    i32x8 x[4][NT];
+  };
+  Next next{int(blockIdx.x), 0};  // the next item to request
+  auto request = [&](Item& f, int slot) {
+    if (next.tile < a.tiles) {
+      issue(next.tile, wave + next.k * waves, slot);
+      load_scales(next.tile, wave + next.k * waves, f.ws);
+    }
+  };
+  Item f0 = {}, f1 = {};
+  request(f0, 0);
 
   // ---- FUSED: the activations into LDS; block kb of row b is unit kb * batch + b ----
   const int batch = a.batch;
@@ -154,7 +169,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
         load16_upto(static_cast<const float*>(a.x) + at, n, x);
     };
     if constexpr (G > 0) {
-      uint32_t* const lds = reinterpret_cast<uint32_t*>(s_mem + kScratch) + wave * kMxWaveLds;
+      uint32_t* const lds = reinterpret_cast<uint32_t*>(ring + (kRingSlots - 1) * kSlot);
       const uint32_t neg = lane_signs<G>(a.signs, lane);
       const int segs = (a.in + 1023) / 1024;  // of a row; the last may end early
       for (int i = wave; i < batch * segs; i += waves) {
@@ -204,46 +219,47 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
     x = i32x8{int(u[0]), int(u[1]), int(u[2]), int(u[3]), int(v[0]), int(v[1]), 0, 0};
   };
 
-  // ---- the stream ----
-  int slot = 0, turn = 0;
-  for (int tile = int(blockIdx.x); tile < a.tiles; tile += int(gridDim.x), turn ^= 1) {
-    f32x4 acc[NT];
+  auto load_xs = [&](Item& f, int chunk) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < mine; ++k) {
-      const int chunk = wave + k * waves;
-      // behind this item's weights: its scales and activations, so that these have
-      // arrived (loads arrive in order) where the weights have
-      uint32_t ws[4];
-      load_scales(tile, chunk, ws);
-      i32x8 x[4][NT];
-      uint32_t xs[4][NT];
+    for (int s = 0; s < 4; ++s)
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+      for (int n = 0; n < NT; ++n)
+        load_x(min(4 * chunk + s, a.stages - 1), n, f.x[s][n], f.xs[s][n]);
+  };
+  load_xs(f0, wave);
+  if (mine == 1) load_xs(f1, wave);  // (one chunk per wave: the same for every tile)
+
+  // ---- the stream: item f in slot `slot`, the next one requested into g ----
+  int tile = int(blockIdx.x), k = 0, turn = 0;
+  f32x4 acc[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) load_x(min(4 * chunk + s, a.stages - 1), n, x[s][n], xs[s][n]);
-      __builtin_amdgcn_sched_barrier(0);
-      request(slot == 0 ? RING - 1 : slot - 1);
-      __builtin_amdgcn_sched_barrier(0);
-      asm volatile("" ::"v"(ws[0]), "v"(ws[1]), "v"(ws[2]), "v"(ws[3]) : "memory");
-      const uint8_t* const w0 = ring + slot * kSlot + r16 * 256;
+  for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto step = [&](Item& f, Item& g, int slot) {
+    advance(next);
+    __builtin_amdgcn_sched_barrier(0);
+    request(g, slot ^ 1);
+    if (mine > 1) load_xs(g, wave + next.k * waves);
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::"v"(f.ws[0]), "v"(f.ws[1]), "v"(f.ws[2]), "v"(f.ws[3]) : "memory");
+    const int chunk = wave + k * waves;
+    const uint8_t* const w0 = ring + slot * kSlot + r16 * 256;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const u32x4 u = *reinterpret_cast<const u32x4*>(w0 + ((4 * s + q) ^ (r16 & 7)) * 16);
-        const i32x8 w = {int(u[0]), int(u[1]), int(u[2]), int(u[3]), 0, 0, 0, 0};
-        if (4 * chunk + s < a.stages) {
+    for (int s = 0; s < 4; ++s) {
+      const u32x4 u = *reinterpret_cast<const u32x4*>(w0 + ((4 * s + q) ^ (r16 & 7)) * 16);
+      const i32x8 w = {int(u[0]), int(u[1]), int(u[2]), int(u[3]), 0, 0, 0, 0};
+      if (4 * chunk + s < a.stages) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-            acc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                x[s][n], w, acc[n], FMT == HIGGS_MX_FP4 ? 4 : 2, 4, 0, int(xs[s][n] >> (8 * q)), 0,
-                int(ws[s] >> (8 * q)));
-        }
+        for (int n = 0; n < NT; ++n)
+          acc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+              f.x[s][n], w, acc[n], FMT == HIGGS_MX_FP4 ? 4 : 2, 4, 0, int(f.xs[s][n] >> (8 * q)),
+              0, int(f.ws[s] >> (8 * q)));
       }
-      // (the slot's reads are done before it is requested again: their data has been
-      // used above)
-      slot = slot == RING - 1 ? 0 : slot + 1;
     }
-    // partial sums: rows 4 q + i of column r16
+    // (the slot's reads are done before it is requested again, in the next step: their
+    // data has been used above)
+    if (++k < mine) return;
+    // the tile's partial sums: rows 4 q + i of column r16
+    k = 0;
     float* const part = reinterpret_cast<float*>(s_mem + kRing + turn * kPart);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -265,11 +281,24 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
           static_cast<float*>(a.y)[at] = t;
       }
     }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    tile += int(gridDim.x);
+    turn ^= 1;
+  };
+  while (true) {
+    step(f0, f1, 0);
+    if (tile >= a.tiles) break;
+    step(f1, f0, 1);
+    if (tile >= a.tiles) break;
   }
 }
 
 template <int FMT, int G, int NT>
-hipError_t launch(const Args& a, int waves, hipStream_t stream) {
+hipError_t launch(const Args& a, hipStream_t stream) {
+  // as few waves as take equal shares of the chunks in as many turns as the most would
+  const int turns = (a.chunks + kMaxWaves - 1) / kMaxWaves;
+  const int waves = (a.chunks + turns - 1) / turns;
   // one block per compute unit, or fewer
   hipLaunchKernelGGL((mx_decode<FMT, G, NT>), dim3(unsigned(std::min(a.tiles, 256))),
                      dim3(unsigned(64 * waves)), 0, stream, a);
@@ -277,17 +306,17 @@ hipError_t launch(const Args& a, int waves, hipStream_t stream) {
 }
 
 template <int FMT>
-hipError_t launch_fmt(const Args& a, int waves, bool fused, int g, hipStream_t stream) {
+hipError_t launch_fmt(const Args& a, bool fused, int g, hipStream_t stream) {
   if (!fused)
-    return a.batch <= 16 ? launch<FMT, -1, 1>(a, waves, stream)
-                         : launch<FMT, -1, 2>(a, waves, stream);
+    return a.batch <= 16 ? launch<FMT, -1, 1>(a, stream)
+                         : launch<FMT, -1, 2>(a, stream);
   switch (g) {
-    case 0: return launch<FMT, 0, 1>(a, waves, stream);
-    case 64: return launch<FMT, 64, 1>(a, waves, stream);
-    case 128: return launch<FMT, 128, 1>(a, waves, stream);
-    case 256: return launch<FMT, 256, 1>(a, waves, stream);
-    case 512: return launch<FMT, 512, 1>(a, waves, stream);
-    default: return launch<FMT, 1024, 1>(a, waves, stream);
+    case 0: return launch<FMT, 0, 1>(a, stream);
+    case 64: return launch<FMT, 64, 1>(a, stream);
+    case 128: return launch<FMT, 128, 1>(a, stream);
+    case 256: return launch<FMT, 256, 1>(a, stream);
+    case 512: return launch<FMT, 512, 1>(a, stream);
+    default: return launch<FMT, 1024, 1>(a, stream);
   }
 }
 
@@ -322,11 +351,8 @@ hipError_t launch_mx_decode(const void* x, higgs_dtype x_dtype, int64_t batch, i
     a.root = 1.0 / std::sqrt(double(g));
     mx_signs(seed, g, &a.signs);
   }
-  // as few waves as take equal shares of the chunks in as many turns as eight would
-  const int turns = (a.chunks + kMaxWaves - 1) / kMaxWaves;
-  const int waves = (a.chunks + turns - 1) / turns;
-  return fmt == HIGGS_MX_FP4 ? launch_fmt<HIGGS_MX_FP4>(a, waves, fused, g, stream)
-                             : launch_fmt<HIGGS_MX_FP6>(a, waves, fused, g, stream);
+  return fmt == HIGGS_MX_FP4 ? launch_fmt<HIGGS_MX_FP4>(a, fused, g, stream)
+                             : launch_fmt<HIGGS_MX_FP6>(a, fused, g, stream);
 }
 
 }  // namespace higgs
