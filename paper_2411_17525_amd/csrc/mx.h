@@ -35,6 +35,13 @@ struct MxTiles {
   int64_t stages;  // of a row: ceil(in / 128), zeros behind `in`
   int64_t rows32;  // rows, rounded up to whole tiles of 32
 };
+// Weight scales for the product: rows x blocks bytes to [stage][rows] words.
+struct MxScaleWords {
+  const uint8_t* from;
+  uint32_t* to;
+  int64_t rows;
+  int blocks, stages;
+};
 constexpr int mx_half_bytes(int fmt) { return fmt == HIGGS_MX_FP4 ? 1024 : 1536; }
 // Offset of the half (1 or 1.5 KiB) that holds block kb of a row.
 template <int FMT>
@@ -46,9 +53,11 @@ __host__ __device__ inline int64_t mx_tile_unit(const MxTiles& t, uint32_t row, 
 hipError_t launch_mx_quantize(const void* w, higgs_dtype dtype, int64_t rows, int64_t in, int fmt,
                               int g, uint64_t seed, uint8_t* codes, uint8_t* scales,
                               hipStream_t stream);
-// The same into the product's order (one launch; batch * in < 2^36).
+// Activations into the product's order (batch * in <= 2^36) and, in the same launch,
+// weight scale words (none where words.to is NULL).
 hipError_t launch_mx_tiles(const void* x, higgs_dtype dtype, int64_t batch, int64_t in, int fmt,
-                           int g, uint64_t seed, const MxTiles& tiles, hipStream_t stream);
+                           int g, uint64_t seed, const MxTiles& tiles, const MxScaleWords& words,
+                           hipStream_t stream);
 hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows,
                                 int64_t in, int fmt, int g, uint64_t seed, void* w,
                                 higgs_dtype dtype, hipStream_t stream);

@@ -379,33 +379,6 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   }
 }
 
-// Weight scales, row after row, to words of a stage's four blocks, stage after
-// stage; zeros behind a row's end. A wave reads 16 bytes each of 64 rows and
-// writes four runs of 64 words.
-__global__ __launch_bounds__(256) void mx_scale_words(const uint8_t* __restrict__ s, int64_t rows,
-                                                      int blocks, int stages,
-                                                      uint32_t* __restrict__ d) {
-  const int64_t row = int64_t(blockIdx.x) * 64 + (threadIdx.x & 63);
-  if (row >= rows) return;
-  const uint8_t* const p = s + row * blocks;
-  for (int t0 = (int(blockIdx.y) * 4 + int(threadIdx.x >> 6)) * 4; t0 < stages;
-       t0 += int(gridDim.y) * 16) {
-    if (t0 * 4 + 16 <= blocks) {
-      typedef uint32_t u32x4_a1 __attribute__((ext_vector_type(4), aligned(1)));
-      const u32x4_a1 u = *reinterpret_cast<const u32x4_a1*>(p + t0 * 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) d[(t0 + i) * rows + row] = u[i];
-    } else {
-      for (int t = t0; t < min(t0 + 4, stages); ++t) {
-        uint32_t w = 0;
-        for (int j = 0; j < 4; ++j)
-          if (t * 4 + j < blocks) w |= uint32_t(p[t * 4 + j]) << (8 * j);
-        d[t * rows + row] = w;
-      }
-    }
-  }
-}
-
 // Sums of the splits in their order, four outputs at a time.
 template <typename OutT>
 __global__ __launch_bounds__(256) void mx_sum_splits(const float* __restrict__ part, int splits,
@@ -524,7 +497,10 @@ hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, 
   Args a{};
   a.x = MxTiles{w, w + p.x_bytes, p.stages, p.rows32};
   hipError_t st = hipSuccess;
-  if (p.x_bytes > 0) st = launch_mx_tiles(x, x_dtype, batch, in, fmt, g, seed, a.x, stream);
+  const MxScaleWords w_scales{scales, p.ws_bytes > 0 ? words : nullptr, out, int(mx_blocks(in)),
+                              int(p.stages)};
+  if (p.x_bytes > 0)
+    st = launch_mx_tiles(x, x_dtype, batch, in, fmt, g, seed, a.x, w_scales, stream);
   if (st != hipSuccess) return st;
   if (p.shape < 0)
     return launch_mx_decode(x, x_dtype, batch, fmt, a.x, codes, scales, g, seed, out, in, y, y_dtype,
@@ -535,12 +511,6 @@ hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, 
   a.batch = batch;
   a.out = out;
   a.blocks = int(mx_blocks(in));
-  hipLaunchKernelGGL(mx_scale_words,
-                     dim3(unsigned((out + 63) / 64),
-                          unsigned(std::min<int64_t>((p.stages + 15) / 16, 64))),
-                     dim3(256), 0, stream, scales, out, a.blocks, int(p.stages), words);
-  st = hipGetLastError();
-  if (st != hipSuccess) return st;
   if (fmt == HIGGS_MX_FP4)
     return y_dtype == HIGGS_F32 ? launch_product<HIGGS_MX_FP4, float>(p, a, part, stream)
                                 : launch_product<HIGGS_MX_FP4, uint16_t>(p, a, part, stream);

@@ -110,9 +110,10 @@ struct TileSink {
 
 // ---- quantization ----
 
-template <int G, int FMT, typename InT, typename Sink>
+template <int G, int FMT, typename InT>
 __global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht(
-    const InT* __restrict__ w, int64_t total, const MxSigns signs, double root, const Sink sink) {
+    const InT* __restrict__ w, int64_t total, const MxSigns signs, double root,
+    const RowSink sink) {
   __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
   uint32_t* const lds = s_lds[wave];
@@ -178,13 +179,125 @@ __global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht_long(
   }
 }
 
+// Weight scales, row after row, to words of a stage's four blocks, stage after
+// stage; zeros behind a row's end. A wave reads 16 bytes each of 64 rows and writes
+// four runs of 64 words. part of parts: its share of the stages.
+__device__ inline void scale_words(const MxScaleWords& s, int64_t rows64, int part, int parts) {
+  const int64_t row = rows64 * 64 + (threadIdx.x & 63);
+  if (row >= s.rows) return;
+  const uint8_t* const p = s.from + row * s.blocks;
+  for (int t0 = (part * (int(blockDim.x) >> 6) + int(threadIdx.x >> 6)) * 4; t0 < s.stages;
+       t0 += parts * (int(blockDim.x) >> 6) * 4) {
+    if (t0 * 4 + 16 <= s.blocks) {
+      typedef uint32_t u32x4_a1 __attribute__((ext_vector_type(4), aligned(1)));
+      const u32x4_a1 u = *reinterpret_cast<const u32x4_a1*>(p + t0 * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s.to[(t0 + i) * s.rows + row] = u[i];
+    } else {
+      for (int t = t0; t < min(t0 + 4, s.stages); ++t) {
+        uint32_t w = 0;
+        for (int j = 0; j < 4; ++j)
+          if (t * 4 + j < s.blocks) w |= uint32_t(p[t * 4 + j]) << (8 * j);
+        s.to[t * s.rows + row] = w;
+      }
+    }
+  }
+}
+
+// Activations into the product's order: a block takes 8 rows x 1024 values, a wave
+// one row's; the codes meet in LDS, so that what goes to memory are runs of 8 rows'
+// units (128 and 64 bytes; written by row they are 16 and 8 bytes apart: 16 us
+// instead of XX for 2048 x 4096 without a rotation). The launch's last
+// blocks put the weights' scales into words.
+constexpr int kTileRows = 8;
+
+template <int G, int FMT, typename InT>
+__global__ __launch_bounds__(64 * kTileRows) void mx_to_tiles(const InT* __restrict__ x, int batch,
+                                                              int in, int segs, int blocks,
+                                                              const MxSigns signs, double root,
+                                                              const MxTiles t,
+                                                              const MxScaleWords words,
+                                                              int word_parts) {
+  // 8 stages x 2 halves x 2 blocks x 8 rows
+  __shared__ __attribute__((aligned(16))) uint8_t s_head[256 * 16];
+  __shared__ __attribute__((aligned(16))) uint8_t s_tail[FMT == HIGGS_MX_FP6 ? 256 * 8 : 16];
+  __shared__ uint32_t s_scale[8 * kTileRows];
+  __shared__ __attribute__((aligned(16))) uint32_t s_lds[G > 0 ? kTileRows : 1][G > 0 ? kMxWaveLds : 4];
+  if (int(blockIdx.x) >= blocks) {
+    const int i = int(blockIdx.x) - blocks;
+    scale_words(words, i / word_parts, i % word_parts, word_parts);
+    return;
+  }
+  const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  const int group = int(blockIdx.x) / segs, seg = int(blockIdx.x) - group * segs;
+  const int row = group * kTileRows + wave, k = 1024 * seg + 16 * lane;
+  if (row < batch) {
+    const int left = in - k;
+    float v[16];
+    load16_upto(x + int64_t(row) * in + (left > 0 ? k : 0), left < 0 ? 0 : left > 16 ? 16 : left, v);
+    uint32_t c[kWords16<FMT>], byte;
+    int block;  // of the segment, whose scale byte this lane holds
+    bool holds;
+    if constexpr (G > 0) {
+      mx_rotate_segment<G, FMT>(v, lane_signs<G>(signs, lane), root, s_lds[wave], lane, c, &byte,
+                                &block);
+      holds = (lane & 15) < 8;
+    } else {
+      byte = mx_plain_halves<FMT>(v, c);
+      block = lane >> 1;
+      holds = (lane & 1) == 0;
+    }
+    // half-block `lane` of the segment: block lane / 2, which is unit (lane / 2) * 8 + row
+    const int unit = (lane >> 1) * kTileRows + wave;
+    uint32_t* const h = reinterpret_cast<uint32_t*>(s_head + unit * 16);
+    if constexpr (FMT == HIGGS_MX_FP4) {
+      *reinterpret_cast<uint2*>(h + (lane & 1) * 2) = make_uint2(c[0], c[1]);
+    } else {
+      uint32_t* const tl = reinterpret_cast<uint32_t*>(s_tail + unit * 8);
+      if ((lane & 1) == 0) {
+        h[0] = c[0];
+        h[1] = c[1];
+        h[2] = c[2];
+      } else {
+        h[3] = c[0];
+        tl[0] = c[1];
+        tl[1] = c[2];
+      }
+    }
+    if (holds)
+      reinterpret_cast<uint8_t*>(s_scale)[((block >> 2) * kTileRows + wave) * 4 + (block & 3)] =
+          uint8_t(byte);
+  }
+  __syncthreads();
+  // unit u = (stage, half, block of the half, row); rows behind the batch are written
+  // too (of their own tile: never read as results)
+  const int stage0 = 8 * seg, stages = min(8, int(t.stages) - stage0);
+  const int r0 = group * kTileRows;
+  uint8_t* const tile = t.codes + (int64_t(r0 / 32) * t.stages + stage0) * 2 * mx_half_bytes(FMT);
+  if (tid < 256) {
+    const int r = tid & 7, blk = tid >> 3;  // blk = 4 stage + 2 half + j
+    if (blk < 4 * stages)
+      *reinterpret_cast<uint4*>(tile + (blk >> 1) * mx_half_bytes(FMT) +
+                                ((blk & 1) * 32 + r0 % 32 + r) * 16) =
+          *reinterpret_cast<const uint4*>(s_head + tid * 16);
+  } else if (FMT == HIGGS_MX_FP6) {
+    const int u = tid - 256, r = u & 7, blk = u >> 3;
+    if (blk < 4 * stages)
+      *reinterpret_cast<uint2*>(tile + (blk >> 1) * mx_half_bytes(FMT) + 1024 +
+                                ((blk & 1) * 32 + r0 % 32 + r) * 8) =
+          *reinterpret_cast<const uint2*>(s_tail + u * 8);
+  }
+  if (tid < 8 * kTileRows && (tid >> 3) < stages)
+    *reinterpret_cast<uint32_t*>(t.scales + ((stage0 + (tid >> 3)) * t.rows32 + r0 + (tid & 7)) * 4) =
+        s_scale[tid];
+}
+
 // No rotation: a lane takes 16 consecutive values, half a block. units: halves
-// of blocks per row; the last block of a row may end early, and blocks behind it
-// (the product's layout has whole stages) are zeros.
-template <int FMT, typename InT, typename Sink>
+// of blocks per row; the last block of a row may end early.
+template <int FMT, typename InT>
 __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__ w, int64_t rows,
                                                          int64_t in, int64_t units,
-                                                         const Sink sink) {
+                                                         const RowSink sink) {
   const int64_t total = rows * units, step = int64_t(gridDim.x) * 256;
   // (total is even, so both halves of a block are in range or neither is)
   for (int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x; u < total; u += step) {
@@ -194,13 +307,8 @@ __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__
     load16_upto(w + row * in + (left > 0 ? k : 0), int(left < 0 ? 0 : left > 16 ? 16 : left), x);
     uint32_t c[kWords16<FMT>];
     const uint32_t byte = mx_plain_halves<FMT>(x, c);
-    if constexpr (std::is_same_v<Sink, TileSink>) {
-      sink.template put_at<FMT>(uint32_t(row), uint32_t(u - row * units), c);
-      if ((u & 1) == 0) sink.put_scale_at(uint32_t(row), uint32_t(u - row * units) >> 1, byte);
-    } else {
-      sink.template put<FMT>(u, c);
-      if ((u & 1) == 0) sink.put_scale(u / 2, byte);
-    }
+    sink.template put<FMT>(u, c);
+    if ((u & 1) == 0) sink.put_scale(u / 2, byte);
   }
 }
 
@@ -481,13 +589,13 @@ void for_group(int g, F f) {
   }
 }
 
-// units: half-blocks per row that the sink holds.
-template <int FMT, typename InT, typename Sink>
-hipError_t quantize_typed(const InT* w, int64_t rows, int64_t in, int64_t units, int g,
-                          uint64_t seed, const Sink& sink, hipStream_t stream) {
+template <int FMT, typename InT>
+hipError_t quantize_typed(const InT* w, int64_t rows, int64_t in, int g, uint64_t seed,
+                          const RowSink& sink, hipStream_t stream) {
   if (g == 0) {
-    hipLaunchKernelGGL((mx_quantize_plain<FMT, InT, Sink>), dim3(unit_blocks(rows * units)),
-                       dim3(256), 0, stream, w, rows, in, units, sink);
+    const int64_t units = 2 * mx_blocks(in);
+    hipLaunchKernelGGL((mx_quantize_plain<FMT, InT>), dim3(unit_blocks(rows * units)), dim3(256),
+                       0, stream, w, rows, in, units, sink);
     return hipGetLastError();
   }
   MxSigns signs;
@@ -497,15 +605,53 @@ hipError_t quantize_typed(const InT* w, int64_t rows, int64_t in, int64_t units,
   for_group(g, [&](auto G) {
     constexpr int kG = decltype(G)::value;
     if constexpr (kG <= 1024) {
-      hipLaunchKernelGGL((mx_quantize_rht<kG, FMT, InT, Sink>),
+      hipLaunchKernelGGL((mx_quantize_rht<kG, FMT, InT>),
                          dim3(wave_blocks((total + 1023) / 1024)), dim3(64 * kWaves), 0, stream, w,
                          total, signs, root, sink);
     } else {
-      hipLaunchKernelGGL((mx_quantize_rht_long<kG / 64, FMT, InT, Sink>),
+      hipLaunchKernelGGL((mx_quantize_rht_long<kG / 64, FMT, InT, RowSink>),
                          dim3(wave_blocks(total / kG)), dim3(64 * kWaves), 0, stream, w, total,
                          signs, root, sink);
     }
   });
+  return hipGetLastError();
+}
+
+template <int FMT, typename InT>
+hipError_t tiles_typed(const InT* x, int64_t batch, int64_t in, int g, uint64_t seed,
+                       const MxTiles& t, const MxScaleWords& words, hipStream_t stream) {
+  MxSigns signs;
+  double root = 0.0;
+  if (g > 0) {
+    mx_signs(seed, g, &signs);
+    root = 1.0 / std::sqrt(double(g));
+  }
+  const int segs = int((in + 1023) / 1024);
+  int64_t blocks = (batch + kTileRows - 1) / kTileRows * segs;
+  if (g > 1024) {  // a wave per group, straight to memory
+    for_group(g, [&](auto G) {
+      constexpr int kG = decltype(G)::value;
+      if constexpr (kG > 1024)
+        hipLaunchKernelGGL((mx_quantize_rht_long<kG / 64, FMT, InT, TileSink>),
+                           dim3(wave_blocks(batch * in / kG)), dim3(64 * kWaves), 0, stream, x,
+                           batch * in, signs, root, TileSink{t, uint32_t(in / 16)});
+    });
+    blocks = 0;
+  }
+  const int parts = int(std::min<int64_t>((words.stages + 31) / 32, 64));
+  const int64_t word_blocks = words.to == nullptr ? 0 : (words.rows + 63) / 64 * parts;
+  if (blocks + word_blocks == 0) return hipGetLastError();
+  const auto launch = [&](auto G) {
+    constexpr int kG = decltype(G)::value;
+    if constexpr (kG <= 1024)
+      hipLaunchKernelGGL((mx_to_tiles<kG, FMT, InT>), dim3(unsigned(blocks + word_blocks)),
+                         dim3(64 * kTileRows), 0, stream, x, int(batch), int(in), segs,
+                         int(blocks), signs, root, t, words, parts);
+  };
+  if (g == 0 || g > 1024)
+    launch(std::integral_constant<int, 0>{});
+  else
+    for_group(g, launch);
   return hipGetLastError();
 }
 
@@ -565,32 +711,31 @@ hipError_t error_typed(const InT* w, int64_t out, int64_t in, const uint8_t* cod
 
 }  // namespace
 
-template <typename Sink>
-static hipError_t quantize_any(const void* w, higgs_dtype dtype, int64_t rows, int64_t in,
-                               int64_t units, int fmt, int g, uint64_t seed, const Sink& sink,
-                               hipStream_t stream) {
-  const float* wf = static_cast<const float*>(w);
-  const uint16_t* wb = static_cast<const uint16_t*>(w);
-  if (fmt == HIGGS_MX_FP4)
-    return dtype == HIGGS_F32
-               ? quantize_typed<HIGGS_MX_FP4>(wf, rows, in, units, g, seed, sink, stream)
-               : quantize_typed<HIGGS_MX_FP4>(wb, rows, in, units, g, seed, sink, stream);
-  return dtype == HIGGS_F32
-             ? quantize_typed<HIGGS_MX_FP6>(wf, rows, in, units, g, seed, sink, stream)
-             : quantize_typed<HIGGS_MX_FP6>(wb, rows, in, units, g, seed, sink, stream);
-}
-
 hipError_t launch_mx_quantize(const void* w, higgs_dtype dtype, int64_t rows, int64_t in, int fmt,
                               int g, uint64_t seed, uint8_t* codes, uint8_t* scales,
                               hipStream_t stream) {
-  return quantize_any(w, dtype, rows, in, 2 * mx_blocks(in), fmt, g, seed,
-                      RowSink{codes, scales}, stream);
+  const float* wf = static_cast<const float*>(w);
+  const uint16_t* wb = static_cast<const uint16_t*>(w);
+  const RowSink sink{codes, scales};
+  if (fmt == HIGGS_MX_FP4)
+    return dtype == HIGGS_F32 ? quantize_typed<HIGGS_MX_FP4>(wf, rows, in, g, seed, sink, stream)
+                              : quantize_typed<HIGGS_MX_FP4>(wb, rows, in, g, seed, sink, stream);
+  return dtype == HIGGS_F32 ? quantize_typed<HIGGS_MX_FP6>(wf, rows, in, g, seed, sink, stream)
+                            : quantize_typed<HIGGS_MX_FP6>(wb, rows, in, g, seed, sink, stream);
 }
 
 hipError_t launch_mx_tiles(const void* x, higgs_dtype dtype, int64_t batch, int64_t in, int fmt,
-                           int g, uint64_t seed, const MxTiles& tiles, hipStream_t stream) {
-  return quantize_any(x, dtype, batch, in, g == 0 ? 8 * tiles.stages : 2 * mx_blocks(in), fmt, g,
-                      seed, TileSink{tiles, uint32_t(in / 16)}, stream);
+                           int g, uint64_t seed, const MxTiles& tiles, const MxScaleWords& words,
+                           hipStream_t stream) {
+  const float* xf = static_cast<const float*>(x);
+  const uint16_t* xb = static_cast<const uint16_t*>(x);
+  if (fmt == HIGGS_MX_FP4)
+    return dtype == HIGGS_F32
+               ? tiles_typed<HIGGS_MX_FP4>(xf, batch, in, g, seed, tiles, words, stream)
+               : tiles_typed<HIGGS_MX_FP4>(xb, batch, in, g, seed, tiles, words, stream);
+  return dtype == HIGGS_F32
+             ? tiles_typed<HIGGS_MX_FP6>(xf, batch, in, g, seed, tiles, words, stream)
+             : tiles_typed<HIGGS_MX_FP6>(xb, batch, in, g, seed, tiles, words, stream);
 }
 
 hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows,
