@@ -93,7 +93,10 @@ __device__ inline float mx_scale_value(uint32_t byte) {
 __device__ inline float mx_odd_f32(double v) {
   const uint64_t u = __builtin_bit_cast(uint64_t, v);
   const uint32_t lo = uint32_t(u), hi = uint32_t(u >> 32);
-  return float(__builtin_bit_cast(double, uint64_t(hi | (lo < 1u ? lo : 1u)) << 32));
+  // (as an instruction: the compiler makes a comparison and a selection of it)
+  uint32_t any;
+  asm("v_min_u32 %0, 1, %1" : "=v"(any) : "v"(lo));
+  return float(__builtin_bit_cast(double, uint64_t(hi | any) << 32));
 }
 
 // 16 scaled values (|v| < 8) to codes, rounded to nearest with ties to even and

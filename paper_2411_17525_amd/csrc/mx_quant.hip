@@ -10,7 +10,7 @@
 // codes are those of the exact rotation.
 //
 // With a rotation, a wavefront takes segments of 1024 values (of g for g =
-// 2048 and 4096): 16 consecutive values per lane, rotated by fwht_rows, which
+// 2048 and 4096): 16 consecutive values per lane, rotated by mx_fwht_rows, which
 // leaves a block in the 16 lanes of a DPP row and two registers. Rows are whole
 // groups there, so the matrix is one run of groups.
 
@@ -157,19 +157,25 @@ __global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht_long(
       for (int i = 0; i < 16; ++i) v[16 * q + i] = double((neg >> i) & 1 ? -x[i] : x[i]);
     }
     fwht_wave<E>(v, lane, 64 * E);
+    constexpr int kShift = kRootShift<64 * E>;
+    if constexpr (kShift == 0) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = normalised(v[i], root);
+      for (int i = 0; i < E; ++i) v[i] *= root;
+    }
 #pragma unroll
     for (int b = 0; b < E / 32; ++b) {
-      uint32_t f = 0;
+      int f = 0;
 #pragma unroll
       for (int i = 0; i < 32; ++i) f = max(f, field_f64(v[32 * b + i]));
-      const uint32_t byte = scale_byte_f64(f);
+      f -= kShift;
+      const bool bad = f >= kMxBad;
+      const int byte = bad ? 255 : scale_exponent_f64(f);
+      const double inverse = inverse_scale(byte, kShift);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float x[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = odd_scaled(v[32 * b + 16 * h + i], byte);
+        for (int i = 0; i < 16; ++i) x[i] = bad ? 0.f : odd_scaled(v[32 * b + 16 * h + i], inverse);
         uint32_t c[kWords16<FMT>];
         mx_encode16<FMT>(x, c);
         sink.template put<FMT>(at / 16 + 2 * b + h, c);
@@ -337,7 +343,7 @@ __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht(
     double v[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = double(x[i]) * double(scale);
-    fwht_rows<G>(v, lds, lane);
+    mx_fwht_rows<G>(v, lds, lane);
 #pragma unroll
     for (int r = 0; r < 16; ++r) x[r] = float(v[r] * root);
     rows_to_lanes<G>(x, reinterpret_cast<float*>(lds), lane);
@@ -452,13 +458,13 @@ __global__ __launch_bounds__(64 * kWaves) void mx_error_rht(
       for (int i = 0; i < 16; ++i) x[i] = 0.f;
     }
     double v[16];
-    signed_f64<G>(x, neg, v);
+    signed_f64(x, neg, v);
 #pragma unroll
     for (int i = 0; i < 16; ++i) norm = __builtin_fma(v[i], v[i], norm);
     mx_decode16<HIGGS_MX_FP4>(c, x);
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] *= scale;
-    fwht_rows<G>(v, lds, lane);
+    mx_fwht_rows<G>(v, lds, lane);
     lanes_to_rows<G>(x, reinterpret_cast<float*>(lds), lane);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
