@@ -79,13 +79,6 @@ hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, 
 
 // ---- device: one value ----
 
-// 2^e for e in [-126, 127] as fp32, or the E8M0 byte's power of two (0 is
-// 2^-127, a subnormal; 255 is NaN).
-__device__ inline float mx_scale_value(uint32_t byte) {
-  if (byte == 255) return __builtin_bit_cast(float, 0x7fc00000u);
-  return __builtin_bit_cast(float, byte == 0 ? 0x00400000u : byte << 23);
-}
-
 // A double rounded to 21 significant bits towards zero with the last bit set
 // where anything was dropped (round to odd), as fp32: rounding that again to
 // nearest, ties to even, to any format of up to 19 bits gives what one rounding
@@ -129,31 +122,29 @@ __device__ inline void mx_encode16(const float (&v)[16], uint32_t* out) {
   }
 }
 
-// The value of an E2M1 / E2M3 code (its low 4 / 6 bits) as fp32.
+// The values of 16 codes (2 or 3 words, least significant bits first) of a block with
+// scale byte `byte`, exact (below 2^-126 too; byte 255: NaN).
 template <int FMT>
-__device__ inline float mx_code_value(uint32_t code) {
-  constexpr int kMan = FMT == HIGGS_MX_FP4 ? 1 : 3;
-  const uint32_t mag = code & ((4u << kMan) - 1);
-  // exponent field e and mantissa m: 2^(e-1) (1 + m 2^-kMan), or m 2^-kMan for
-  // e = 0; as an fp32 pattern moved down by 2^126, the subnormal case is one too
-  const float v = __builtin_bit_cast(float, mag << (23 - kMan)) *
-                  __builtin_bit_cast(float, 253u << 23);  // 2^126
-  return (code >> (kMan + 2)) & 1 ? -v : v;
-}
-
-// 16 codes (2 or 3 words, least significant bits first) to fp32 values.
-template <int FMT>
-__device__ inline void mx_decode16(const uint32_t* in, float (&v)[16]) {
+__device__ inline void mx_decode16(const uint32_t* in, uint32_t byte, float (&v)[16]) {
+  // (the instructions take the exponent field of the scale: 0 is 2^-127, 255 NaN)
+  const float scale = __builtin_bit_cast(float, byte << 23);
+  if constexpr (FMT == HIGGS_MX_FP4) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    if constexpr (FMT == HIGGS_MX_FP4) {
-      v[i] = mx_code_value<FMT>(in[i / 8] >> (4 * (i % 8)));
-    } else {
-      const int bit = 6 * i, w = bit / 32, s = bit % 32;
-      uint32_t c = in[w] >> s;
-      if (s > 26) c |= in[w + 1] << (32 - s);
-      v[i] = mx_code_value<FMT>(c);
+    for (int h = 0; h < 2; ++h) {
+      const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(in[h], scale, 0);
+      const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(in[h], scale, 1);
+      const auto c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(in[h], scale, 2);
+      const auto d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(in[h], scale, 3);
+      float* const o = v + 8 * h;
+      o[0] = a[0], o[1] = a[1], o[2] = b[0], o[3] = b[1];
+      o[4] = c[0], o[5] = c[1], o[6] = d[0], o[7] = d[1];
     }
+  } else {
+    typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
+    const auto r =
+        __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(u32x6{in[0], in[1], in[2], 0, 0, 0}, scale);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = r[i];
   }
 }
 

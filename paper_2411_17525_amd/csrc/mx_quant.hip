@@ -320,35 +320,31 @@ __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__
 
 // ---- the way back ----
 
+// Rotated back in fp32 (stored values are not decided at borders): 16 consecutive
+// values per lane throughout, butterflies over lanes by DPP and permlane, no LDS.
 template <int G, int FMT, typename OutT>
 __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht(
     const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t total,
-    const MxSigns signs, double root, OutT* __restrict__ w) {
-  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds];
+    const MxSigns signs, float root, OutT* __restrict__ w) {
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  uint32_t* const lds = s_lds[wave];
   const uint32_t neg = lane_signs<G>(signs, lane);
   const int64_t segs = (total + 1023) / 1024, step = int64_t(gridDim.x) * kWaves;
   for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
     const int64_t at = 1024 * seg + 16 * lane;
     const bool live = at < total;
-    uint32_t c[kWords16<FMT>] = {};
-    float scale = 0.f;
+    uint32_t c[kWords16<FMT>] = {}, byte = 0;
     if (live) {
       load_codes16<FMT>(codes + (at / 16) * (4 * kWords16<FMT>), c);
-      scale = mx_scale_value(scales[at / 32]);
+      byte = scales[at / 32];
     }
     float x[16];
-    mx_decode16<FMT>(c, x);
-    double v[16];
+    mx_decode16<FMT>(c, byte, x);
+    fwht_in_lane<16>(x);
+    const float s = fwht_cross_lane_deferred_fixed<16, G>(x, lane) * root;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = double(x[i]) * double(scale);
-    mx_fwht_rows<G>(v, lds, lane);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = float(v[r] * root);
-    rows_to_lanes<G>(x, reinterpret_cast<float*>(lds), lane);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = (neg >> i) & 1 ? -x[i] : x[i];
+    for (int i = 0; i < 16; ++i)
+      x[i] = __builtin_bit_cast(
+          float, __builtin_bit_cast(uint32_t, x[i] * s) ^ ((neg << (31 - i)) & 0x80000000u));
     if (live) store16(w + at, x);
   }
 }
@@ -356,33 +352,32 @@ __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht(
 template <int E, int FMT, typename OutT>
 __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht_long(
     const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t total,
-    const MxSigns signs, double root, OutT* __restrict__ w) {
+    const MxSigns signs, float root, OutT* __restrict__ w) {
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
   const int64_t segs = total / (64 * E), step = int64_t(gridDim.x) * kWaves;
   for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
     const int64_t at = 64 * E * seg + E * lane;
-    double v[E];
+    float v[E];
 #pragma unroll
     for (int q = 0; q < E / 16; ++q) {
       uint32_t c[kWords16<FMT>];
       load_codes16<FMT>(codes + (at / 16 + q) * (4 * kWords16<FMT>), c);
-      const double scale = double(mx_scale_value(scales[(at + 16 * q) / 32]));
       float x[16];
-      mx_decode16<FMT>(c, x);
+      mx_decode16<FMT>(c, scales[(at + 16 * q) / 32], x);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[16 * q + i] = double(x[i]) * scale;
+      for (int i = 0; i < 16; ++i) v[16 * q + i] = x[i];
     }
-    fwht_wave<E>(v, lane, 64 * E);
+    fwht_in_lane<E>(v);
+    const float s = fwht_cross_lane_deferred_fixed<E, 64 * E>(v, lane) * root;
 #pragma unroll
     for (int q = 0; q < E / 16; ++q) {
       const int j = E * lane + 16 * q;
       const uint32_t neg = signs.w[j >> 5] >> (j & 16);
       float x[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float f = float(v[16 * q + i] * root);
-        x[i] = (neg >> i) & 1 ? -f : f;
-      }
+      for (int i = 0; i < 16; ++i)
+        x[i] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v[16 * q + i] * s) ^
+                                             ((neg << (31 - i)) & 0x80000000u));
       store16(w + at + 16 * q, x);
     }
   }
@@ -400,11 +395,8 @@ __global__ __launch_bounds__(256) void mx_dequantize_plain(const uint8_t* __rest
     if (left <= 0) continue;  // the second half of a row's last block
     uint32_t c[kWords16<FMT>];
     load_codes16<FMT>(codes + u * (4 * kWords16<FMT>), c);
-    const float scale = mx_scale_value(scales[u / 2]);
     float x[16];
-    mx_decode16<FMT>(c, x);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] *= scale;
+    mx_decode16<FMT>(c, scales[u / 2], x);
     store16_upto(w + row * in + k, int(left > 16 ? 16 : left), x);
   }
 }
@@ -447,12 +439,11 @@ __global__ __launch_bounds__(64 * kWaves) void mx_error_rht(
     const int64_t at = k0 + 16 * lane;
     const bool live = at < in;
     float x[16];
-    uint32_t c[2] = {0, 0};
-    float scale = 0.f;
+    uint32_t c[2] = {0, 0}, byte = 0;
     if (live) {
       load16(wr + at, x);
       load_codes16<HIGGS_MX_FP4>(cr + at / 2, c);
-      scale = mx_scale_value(sr[at / 32]);
+      byte = sr[at / 32];
     } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = 0.f;
@@ -461,9 +452,7 @@ __global__ __launch_bounds__(64 * kWaves) void mx_error_rht(
     signed_f64(x, neg, v);
 #pragma unroll
     for (int i = 0; i < 16; ++i) norm = __builtin_fma(v[i], v[i], norm);
-    mx_decode16<HIGGS_MX_FP4>(c, x);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] *= scale;
+    mx_decode16<HIGGS_MX_FP4>(c, byte, x);
     mx_fwht_rows<G>(v, lds, lane);
     lanes_to_rows<G>(x, reinterpret_cast<float*>(lds), lane);
 #pragma unroll
@@ -503,12 +492,11 @@ __global__ __launch_bounds__(64 * kWaves) void mx_error_rht_long(
     for (int q = 0; q < E / 16; ++q) {
       uint32_t c[2];
       load_codes16<HIGGS_MX_FP4>(codes + (at + 16 * q) / 2, c);
-      const float scale = mx_scale_value(scales[(at + 16 * q) / 32]);
       float x[16];
-      mx_decode16<HIGGS_MX_FP4>(c, x);
+      mx_decode16<HIGGS_MX_FP4>(c, scales[(at + 16 * q) / 32], x);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const double d = __builtin_fma(v[16 * q + i], root, -double(x[i] * scale));
+        const double d = __builtin_fma(v[16 * q + i], root, -double(x[i]));
         err = __builtin_fma(d, d, err);
       }
     }
@@ -533,12 +521,11 @@ __global__ __launch_bounds__(64 * kWaves) void mx_error_plain(const InT* __restr
     load16_upto(w + row * in + 16 * u, n, x);
     uint32_t c[2];
     load_codes16<HIGGS_MX_FP4>(codes + (row * units + u) * 8, c);
-    const float scale = mx_scale_value(scales[(row * units + u) / 2]);
-    mx_decode16<HIGGS_MX_FP4>(c, q);
+    mx_decode16<HIGGS_MX_FP4>(c, scales[(row * units + u) / 2], q);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (i < n) {
-        const double v = double(x[i]), d = v - double(q[i] * scale);
+        const double v = double(x[i]), d = v - double(q[i]);
         norm = __builtin_fma(v, v, norm);
         err = __builtin_fma(d, d, err);
       }
@@ -672,7 +659,7 @@ hipError_t dequantize_typed(const uint8_t* codes, const uint8_t* scales, int64_t
   }
   MxSigns signs;
   mx_signs(seed, g, &signs);
-  const double root = 1.0 / std::sqrt(double(g));
+  const float root = float(1.0 / std::sqrt(double(g)));
   const int64_t total = rows * in;
   for_group(g, [&](auto G) {
     constexpr int kG = decltype(G)::value;
