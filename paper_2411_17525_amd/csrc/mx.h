@@ -32,7 +32,7 @@ void mx_signs(uint64_t seed, int g, MxSigns* s);
 struct MxTiles {
   uint8_t* codes;
   uint8_t* scales;
-  int64_t stages;  // of a row: ceil(in / 128), zeros behind `in`
+  int64_t stages;  // of a row: an even number, 2 ceil(in / 256), zeros behind `in`
   int64_t rows32;  // rows, rounded up to whole tiles of 32
 };
 // Weight scales for the product: rows x blocks bytes to [stage][rows] words.

@@ -78,12 +78,12 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
   const __amdgpu_buffer_rsrc_t wrs = rsrc(a.wc, uint32_t(a.out * a.blocks * 16));
   uint8_t* const ring = s_mem + wave * kWaveRing;
   const int mine = (a.chunks - wave + waves - 1) / waves;  // chunks wave, wave + waves, ..
-  // 4 rows of 256 bytes per load; a row's 16 blocks are permuted so that eight rows of
-  // one block lie in distinct banks
+  // 4 rows of 256 bytes per load; a row's 16 blocks are permuted so that 16 rows of one
+  // block lie in distinct banks
   auto issue = [&](int tile, int chunk, int slot) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int row = 4 * j + q, unit = r16 ^ (row & 7);
+      const int row = 4 * j + q, unit = r16 ^ row;
       const uint32_t at = uint32_t(min(int64_t(tile) * 16 + row, a.out - 1)) * uint32_t(a.blocks * 16) +
                           uint32_t(chunk * 256 + unit * 16);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(wrs, (lds_void*)(ring + slot * kSlot + j * 1024), 16,
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
     const uint8_t* const w0 = ring + slot * kSlot + r16 * 256;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const u32x4 u = *reinterpret_cast<const u32x4*>(w0 + ((4 * s + q) ^ (r16 & 7)) * 16);
+      const u32x4 u = *reinterpret_cast<const u32x4*>(w0 + ((4 * s + q) ^ r16) * 16);
       const i32x8 w = {int(u[0]), int(u[1]), int(u[2]), int(u[3]), 0, 0, 0, 0};
       if (4 * chunk + s < a.stages) {
 #pragma unroll

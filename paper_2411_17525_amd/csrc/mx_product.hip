@@ -60,15 +60,17 @@ __device__ MX_INLINE inline void for_each(const F& f) {
   }
 }
 
-// A block computes BM activation rows x BN outputs over a range of K with WM x WN
-// waves, stage by stage of 128 values: the stage's activations, weights and scale
+// A block computes tiles of BM activation rows x BN outputs over a range of K with
+// WM x WN waves, one after another, stage by stage of 128 values: the stage's activations, weights and scale
 // words go from memory to LDS, from there into the operands. The loads run NB - 1/2
 // stages ahead. Weights are loaded for two stages at a time, 128 bytes of a
 // row: the address unit takes about as long for half a line as for a whole one
 // (62, 88 and 106 GB/s per compute unit in pieces of 64, 128 and 256 bytes), and
 // that time is what the products have to hide. So that every stage loads as much,
 // the block's first half of columns has its pairs of stages at (0, 1), (2, 3) ..,
-// the second at (-1, 0), (1, 2) .. (NB is odd). A stage is computed in halves; the
+// the second at (-1, 0), (1, 2) .. (NB is odd; a range of K has an even number of
+// stages). The loads run on into the next tile, so that its first stages arrive while
+// this one's outputs are stored. A stage is computed in halves; the
 // operands of a half are read while the other half is multiplied, and the one
 // barrier of a stage stands between its halves: there the next stage has landed
 // and this one has been read by all waves.
@@ -87,7 +89,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   // loads of 1 KiB (codes) and 256 bytes (scales) per stage, and per wave; a wave
   // without one repeats the last
   constexpr int kXLoads = kXBytes / 1024, kWLoads = kPair / 1024, kSLoads = (kXRows + BN) / 64;
-  constexpr int kXPer = (kXLoads + kWaves - 1) / kWaves, kWPer = (kWLoads + kWaves - 1) / kWaves;
+  constexpr int kXPer = (kXLoads + kWaves - 1) / kWaves, kWPer = kWLoads / kWaves;
   constexpr int kSPer = (kSLoads + kWaves - 1) / kWaves, kLoads = kXPer + kSPer + kWPer;
   static_assert(BM % 32 == 0 && BN % 64 == 0 && NB % 2 == 1 && NB >= 3, "tile");
   static_assert(PERCU * kLds <= 160 * 1024 && (NB - 1) * kLoads + kWPer < 64, "tile");
@@ -98,87 +100,135 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   const int wm = wave % WM, wn = wave / WM;
   const int r32 = lane & 31, hi = lane >> 5;
 
-  // ---- the block's tile: consecutive tiles per XCD, eight row tiles of one column
-  //      after another (their weights stay in the XCD's L2) ----
+  // ---- the block's tiles: consecutive ones per XCD, dealt to its blocks in turn; eight
+  //      row tiles of one column after another (their weights stay in the XCD's L2) ----
   const int total = a.mtiles * a.ntiles * a.splits;
-  const int xcd = int(blockIdx.x) % 8, turn = int(blockIdx.x) / 8;
-  const int item = xcd * (total / 8) + min(xcd, total % 8) + turn;
-  const int split = item / (a.mtiles * a.ntiles);
-  const int tile = item - split * (a.mtiles * a.ntiles);
-  constexpr int kBand = 8;
-  const int band = tile / (kBand * a.ntiles), rest = tile - band * (kBand * a.ntiles);
-  const int high = min(kBand, a.mtiles - band * kBand);
-  const int nt = rest / high, mt = band * kBand + rest - nt * high;
-  const int64_t m0 = int64_t(mt) * BM, n0 = int64_t(nt) * BN;
+  const int xcd = int(blockIdx.x) % 8, step = (int(gridDim.x) + 7) / 8;  // (its blocks)
+  const int end = (xcd + 1) * (total / 8) + min(xcd + 1, total % 8);
+  struct Tile {
+    int item, mt, nt, split, first, count;
+  };
   const int stages = int(a.x.stages);
-  const int pairs = (stages + 1) / 2;  // (splits begin at whole pairs: whole lines)
-  const int first = pairs * split / a.splits * 2;
-  const int count = min(pairs * (split + 1) / a.splits * 2, stages) - first;
+  auto locate = [&](int item) MX_INLINE {
+    auto uniform = [](int v) MX_INLINE { return __builtin_amdgcn_readfirstlane(v); };
+    Tile r;
+    r.item = item;
+    r.split = uniform(item / (a.mtiles * a.ntiles));
+    const int tile = item - r.split * (a.mtiles * a.ntiles);
+    constexpr int kBand = 8;
+    const int band = uniform(tile / (kBand * a.ntiles)), rest = tile - band * (kBand * a.ntiles);
+    const int high = min(kBand, a.mtiles - band * kBand);
+    r.nt = uniform(rest / high);
+    r.mt = band * kBand + rest - r.nt * high;
+    r.first = uniform(stages / 2 * r.split / a.splits) * 2;
+    r.count = uniform(stages / 2 * (r.split + 1) / a.splits) * 2 - r.first;
+    return r;
+  };
+  Tile now = locate(xcd * (total / 8) + min(xcd, total % 8) + int(blockIdx.x) / 8);
 
-  // ---- loads of a stage ----
-  const int mrows = int(min(int64_t(BM), a.x.rows32 - m0));   // a multiple of 32
-  const int nrows = int(min(int64_t(BN), a.out - n0));
-  // sizes in bytes of what the block may read; 0 for the loads of stages past the
-  // end, which then read nothing (every stage issues the same number of loads, for
-  // the waits count them)
-  const uint8_t* const xp = a.x.codes + (m0 / 32 * stages + first) * kTile;
-  const uint8_t* const wp = a.wc + n0 * a.blocks * 16;
-  const uint8_t* const xsp = a.x.scales + (first * a.x.rows32 + m0) * 4;
-  const uint32_t* const wsp = a.ws + first * a.out + n0;
-  const uint32_t xbytes = uint32_t(((mrows / 32 - 1) * stages + count) * kTile);
-  const uint32_t wbytes = uint32_t(nrows * a.blocks * 16);
-  const uint32_t xsbytes = uint32_t(((count - 1) * a.x.rows32 + mrows) * 4);
-  const uint32_t wsbytes = uint32_t(((count - 1) * a.out + nrows) * 4);
+  // ---- loads: stage `lstage` of tile `ltile`, ahead of the products. Past the last tile
+  //      they read nothing (no records, or offsets out of range), but are issued: the
+  //      waits count them ----
+  Tile ltile = now;
+  int lstage = 0;
+  constexpr uint32_t kNowhere = 0xC0000000u;  // (codes are below 2 GiB)
+  const __amdgpu_buffer_rsrc_t wrs = rsrc(a.wc, uint32_t(a.out * a.blocks * 16));
+  const uint8_t *xp, *xsp;
+  const uint32_t* wsp;
+  uint32_t xbytes, xsbytes, wsbytes;
   uint32_t xoff[kXPer], woff[2][kWPer], soff[kSPer];  // (woff[0]: of the next stage's half)
+  // 8 rows of 128 bytes per load; a row's eight blocks are permuted so that 16 rows of
+  // one block lie in distinct banks (of 64, two rows)
+  static_assert(kWLoads % kWaves == 0 && kWaves % 2 == 0, "row = 8 wave + lane / 8 mod 16");
+  const int wunit = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
+  auto row_offset = [&](const Tile& t, int i, int side) MX_INLINE {
+    const int row = (wave + i * kWaves) * 8 + lane / 8 + side * (BN / 2);
+    const int64_t o = min(int64_t(t.nt) * BN + row, a.out - 1);
+    // (the second half's first pair begins a stage early: what that reads is not used)
+    return uint32_t(o) * uint32_t(a.blocks * 16) + uint32_t(t.first * 64 + wunit * 16 - side * 64);
+  };
+  auto begin_tile = [&] MX_INLINE {  // activations and scales of ltile from its first stage
+    const bool live = ltile.item < end;
+    const int64_t m0 = int64_t(ltile.mt) * BM, n0 = int64_t(ltile.nt) * BN;
+    const int mrows = int(min(int64_t(BM), a.x.rows32 - m0));  // a multiple of 32
+    const int nrows = int(min(int64_t(BN), a.out - n0));
+    xp = a.x.codes + (m0 / 32 * stages + ltile.first) * kTile;
+    xsp = a.x.scales + (ltile.first * a.x.rows32 + m0) * 4;
+    wsp = a.ws + ltile.first * a.out + n0;
+    xbytes = live ? uint32_t(((mrows / 32 - 1) * stages + ltile.count) * kTile) : 0;
+    xsbytes = live ? uint32_t(((ltile.count - 1) * a.x.rows32 + mrows) * 4) : 0;
+    wsbytes = live ? uint32_t(((ltile.count - 1) * a.out + nrows) * 4) : 0;
 #pragma unroll
-  for (int i = 0; i < kXPer; ++i) {
-    const int j = min(wave + i * kWaves, kXLoads - 1);
-    const int at = j * 1024 + lane * 16, t = min(at / kTile, mrows / 32 - 1);
-    xoff[i] = uint32_t(t * stages * kTile + at % kTile);
-  }
+    for (int i = 0; i < kXPer; ++i) {
+      const int j = min(wave + i * kWaves, kXLoads - 1);
+      const int at = j * 1024 + lane * 16, t = min(at / kTile, mrows / 32 - 1);
+      xoff[i] = uint32_t(t * stages * kTile + at % kTile);
+    }
+#pragma unroll
+    for (int i = 0; i < kSPer; ++i) {
+      const int j = min(wave + i * kWaves, kSLoads - 1);
+      soff[i] = j < kXRows / 64 ? uint32_t(min(j * 64 + lane, mrows - 1) * 4)
+                                : uint32_t(min((j - kXRows / 64) * 64 + lane, nrows - 1) * 4);
+    }
+  };
+  begin_tile();
 #pragma unroll
   for (int i = 0; i < kWPer; ++i) {
-    // 8 rows of 128 bytes; a row's eight blocks are permuted so that eight rows of
-    // one block lie in distinct banks
-    const int row = min(wave + i * kWaves, kWLoads - 1) * 8 + lane / 8;
-    const int at = first * 64 + ((lane & 7) ^ (row & 7)) * 16;
-    woff[1][i] = uint32_t(min(row, nrows - 1) * a.blocks * 16 + at);
-    // (its first pair begins a stage early: what that reads is not used, below the
-    // buffer's start it is out of range)
-    woff[0][i] = uint32_t(min(row + BN / 2, nrows - 1) * a.blocks * 16 + at - 64);
+    woff[0][i] = row_offset(now, i, 1);
+    woff[1][i] = row_offset(now, i, 0);
   }
+  // Before the loads of a tile's last stage: the second columns' pair that it begins
+  // ends with the next tile's first stage (the upper four blocks of each row).
+  uint32_t cross[kWPer];
+  auto begin_stage = [&] MX_INLINE {
+    if (lstage != ltile.count - 1) return;
+    const int item = ltile.item + step;
+    if (item < end) {
+      ltile = locate(item);
 #pragma unroll
-  for (int i = 0; i < kSPer; ++i) {
-    const int j = min(wave + i * kWaves, kSLoads - 1);
-    soff[i] = j < kXRows / 64 ? uint32_t(min(j * 64 + lane, mrows - 1) * 4)
-                              : uint32_t(min((j - kXRows / 64) * 64 + lane, nrows - 1) * 4);
-  }
-  // Load k of this wave (constant) for stage t into stage buffer buf and, the weights
-  // of the stage's half of the columns, into its pair buffer lpair; the offsets one
-  // stage or pair on, the weights' exchanged with the other half's.
-  auto issue = [&](auto K, int t, int buf, int lpair) MX_INLINE {
-    const bool live = t < count;
+      for (int i = 0; i < kWPer; ++i) cross[i] = row_offset(ltile, i, 1);
+    } else {
+      ltile.item = item;
+#pragma unroll
+      for (int i = 0; i < kWPer; ++i) cross[i] = kNowhere;
+    }
+    lstage = -1;
+#pragma unroll
+    for (int i = 0; i < kWPer; ++i) woff[0][i] = wunit >= 4 ? cross[i] : woff[0][i];
+  };
+  auto end_stage = [&] MX_INLINE {
+    if (++lstage != 0) return;
+    begin_tile();
+#pragma unroll
+    for (int i = 0; i < kWPer; ++i) {
+      woff[0][i] = ltile.item < end ? row_offset(ltile, i, 0) : kNowhere;
+      woff[1][i] = cross[i] + 128;
+    }
+  };
+  // Load k of this wave (constant) into stage buffer buf and, the weights of column half
+  // `side`, into its pair buffer lpair; the offsets one stage or pair on, the weights'
+  // exchanged with the other half's.
+  auto issue = [&](auto K, int side, int buf, int lpair) MX_INLINE {
     constexpr int k = decltype(K)::value;
     uint8_t* const s = s_mem + buf * kStage;
     if constexpr (k < kXPer) {
       const int j = min(wave + k * kWaves, kXLoads - 1);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(xp, live ? xbytes : 0), (lds_void*)(s + j * 1024),
-                                               16, int(xoff[k]), 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(xp, xbytes), (lds_void*)(s + j * 1024), 16,
+                                               int(xoff[k]), 0, 0, 0);
       xoff[k] += kTile;
     } else if constexpr (k < kXPer + kSPer) {
       constexpr int i = k - kXPer;
       const int j = min(wave + i * kWaves, kSLoads - 1);
       const bool is_x = j < kXRows / 64;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rsrc(is_x ? static_cast<const void*>(xsp) : wsp, live ? is_x ? xsbytes : wsbytes : 0),
+          rsrc(is_x ? static_cast<const void*>(xsp) : wsp, is_x ? xsbytes : wsbytes),
           (lds_void*)(s + kXScale + j * 256), 4, int(soff[i]), 0, 0, 0);
       soff[i] += uint32_t(is_x ? a.x.rows32 : a.out) * 4;
     } else {
       constexpr int i = k - kXPer - kSPer;
-      const int j = min(wave + i * kWaves, kWLoads - 1);
+      const int j = wave + i * kWaves;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rsrc(wp, live ? wbytes : 0),
-          (lds_void*)(s_mem + kWeights + ((t & 1) * kPairs + lpair) * kPair + j * 1024), 16,
+          wrs, (lds_void*)(s_mem + kWeights + (side * kPairs + lpair) * kPair + j * 1024), 16,
           int(woff[0][i]), 0, 0, 0);
       const uint32_t other = woff[1][i];
       woff[1][i] = woff[0][i] + 128;
@@ -189,8 +239,8 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   // ---- operands of half h of the stage in buffer buf ----
   struct Half {
     uint32_t x[TM][6], w[TN][4];
-    uint32_t xs[TM], ws[TN];
   };
+  uint32_t words[TM + TN], scales[TM + TN];  // the next stage's scale words; this one's
   // (the tails' addresses apart: two of them read by one instruction would have to
   // be moved into place)
   uint32_t tail[TM];
@@ -199,38 +249,36 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
     tail[m] = uint32_t((wm * TM + m) * kTile + 1024 + lane * 8);
     asm volatile("" : "+v"(tail[m]));
   }
-  // read k of a half's operands, in the order in which the products need them:
-  // the first row tile, all column tiles, the other row tiles
-  constexpr int kXReads = FMT == HIGGS_MX_FP6 ? 3 : 2;
-  constexpr int kReads = TM * kXReads + TN * 2;
+  // read k of a half's operands, in the order in which the products need them: the
+  // first row tile, all column tiles, the other row tiles; then the scale words
+  constexpr int kXReads = FMT == HIGGS_MX_FP6 ? 2 : 1;
+  constexpr int kReads = TM * kXReads + TN;
   auto read = [&](auto K, Half& f, int t, int buf, int pair0, int pair1, int h) MX_INLINE {
     constexpr int k = decltype(K)::value;
     const uint8_t* const s = s_mem + buf * kStage;
-    if constexpr (k >= kXReads && k < kXReads + TN * 2) {
-      constexpr int n = (k - kXReads) / 2;
+    if constexpr (k >= kReads) {
+      constexpr int q = k - kReads;
+      const int at = q < TM ? kXScale + ((wm * TM + q) * 32 + r32) * 4
+                            : kWScale + ((wn * TN + q - TM) * 32 + r32) * 4;
+      words[q] = *reinterpret_cast<const uint32_t*>(s + at);
+    } else if constexpr (k >= kXReads && k < kXReads + TN) {
+      constexpr int n = k - kXReads;
       const int row = (wn * TN + n) * 32 + r32;
-      if constexpr ((k - kXReads) % 2 == 0) {
-        const int side = row / (BN / 2);  // (the same in all lanes)
-        const int pair = __builtin_amdgcn_readfirstlane(side ? kPairs + pair1 : pair0);
-        const int odd = __builtin_amdgcn_readfirstlane((t + side) & 1);
-        const int unit = (4 * odd + 2 * h + hi) ^ (row & 7);
-        const u32x4 u = *reinterpret_cast<const u32x4*>(
-            s_mem + kWeights + pair * kPair + (row - side * (BN / 2)) * 128 + unit * 16);
+      const int side = row / (BN / 2);  // (the same in all lanes)
+      const int pair = __builtin_amdgcn_readfirstlane(side ? kPairs + pair1 : pair0);
+      const int odd = __builtin_amdgcn_readfirstlane((t + side) & 1);
+      const int unit = (4 * odd + 2 * h + hi) ^ ((row >> 1) & 7);
+      const u32x4 u = *reinterpret_cast<const u32x4*>(
+          s_mem + kWeights + pair * kPair + (row - side * (BN / 2)) * 128 + unit * 16);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f.w[n][i] = u[i];
-      } else {
-        f.ws[n] = *reinterpret_cast<const uint32_t*>(s + kWScale + row * 4);
-      }
+      for (int i = 0; i < 4; ++i) f.w[n][i] = u[i];
     } else {
-      constexpr int q = k < kXReads ? k : k - TN * 2, m = q / kXReads, part = q % kXReads;
+      constexpr int q = k < kXReads ? k : k - TN, m = q / kXReads, part = q % kXReads;
       if constexpr (part == 0) {
         const u32x4 u =
             *reinterpret_cast<const u32x4*>(s + (wm * TM + m) * kTile + h * kHalf + lane * 16);
 #pragma unroll
         for (int i = 0; i < 4; ++i) f.x[m][i] = u[i];
-      } else if constexpr (part == 1) {
-        f.xs[m] =
-            *reinterpret_cast<const uint32_t*>(s + kXScale + ((wm * TM + m) * 32 + r32) * 4);
       } else {
         const u32x2 u = *reinterpret_cast<const u32x2*>(s + tail[m] + h * kHalf);
         f.x[m][4] = u[0];
@@ -243,7 +291,8 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   for (int m = 0; m < TM; ++m)
 #pragma unroll
     for (int n = 0; n < TN; ++n) acc[m][n] = f32x16{};
-  // product k of a half; the scale bytes of half h are byte 2 h + lane / 32 of the words
+  // product k of a half; the scale bytes of half h are byte 2 h + lane / 32 of the words,
+  // moved down by lane / 32 bytes in `scales`
   auto multiply = [&](auto K, const Half& f, auto H) MX_INLINE {
     constexpr int m = decltype(K)::value / TN, n = decltype(K)::value % TN;
     constexpr int h = decltype(H)::value, kFormat = FMT == HIGGS_MX_FP4 ? 4 : 2;
@@ -252,8 +301,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
                      FMT == HIGGS_MX_FP6 ? int(f.x[m][5]) : 0, 0, 0};
     const i32x8 w = {int(f.w[n][0]), int(f.w[n][1]), int(f.w[n][2]), int(f.w[n][3]), 0, 0, 0, 0};
     acc[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-        x, w, acc[m][n], kFormat, 4, 2 * h, int(f.xs[m] >> (8 * hi)), 2 * h,
-        int(f.ws[n] >> (8 * hi)));
+        x, w, acc[m][n], kFormat, 4, 2 * h, int(scales[m]), 2 * h, int(scales[TM + n]));
   };
   using H0 = std::integral_constant<int, 0>;
   using H1 = std::integral_constant<int, 1>;
@@ -267,21 +315,22 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
     int stage, buf, pair0, pair1;  // pair0, pair1: the pair buffers of both column halves
   };
   auto half = [&](const Half& now, auto H, Half& next, const Place& np, int nh, auto L0, auto L1,
-                  int lt, int lbuf, int lpair) MX_INLINE {
+                  int lside, int lbuf, int lpair) MX_INLINE {
     constexpr int kOver = kProducts >= 4 ? kProducts * 3 / 4 : kProducts;
     constexpr int l0 = decltype(L0)::value, nl = decltype(L1)::value - l0;
+    constexpr int kAll = kReads + (decltype(H)::value == 1 ? TM + TN : 0);
     for_each<kProducts>([&](auto I) MX_INLINE {
       constexpr int i = decltype(I)::value;
       multiply(I, now, H);
-      constexpr int ra = kReads * (i < kOver ? i : kOver) / kOver;
-      constexpr int rb = kReads * (i + 1 < kOver ? i + 1 : kOver) / kOver;
+      constexpr int ra = kAll * (i < kOver ? i : kOver) / kOver;
+      constexpr int rb = kAll * (i + 1 < kOver ? i + 1 : kOver) / kOver;
       for_each<rb - ra>([&](auto J) MX_INLINE {
         read(std::integral_constant<int, ra + decltype(J)::value>{}, next, np.stage, np.buf,
              np.pair0, np.pair1, nh);
       });
       constexpr int la = l0 + nl * i / kProducts, lb = l0 + nl * (i + 1) / kProducts;
       for_each<lb - la>([&](auto J) MX_INLINE {
-        issue(std::integral_constant<int, la + decltype(J)::value>{}, lt, lbuf, lpair);
+        issue(std::integral_constant<int, la + decltype(J)::value>{}, lside, lbuf, lpair);
       });
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -294,48 +343,66 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   using LH = std::integral_constant<int, (kLoads + 1) / 2>;
   using LN = std::integral_constant<int, kLoads>;
   for_each<kWPer>([&](auto K) MX_INLINE {  // (the second columns' pair that ends with stage 0)
-    issue(std::integral_constant<int, kXPer + kSPer + decltype(K)::value>{}, -1, 0, 0);
+    issue(std::integral_constant<int, kXPer + kSPer + decltype(K)::value>{}, 1, 0, 0);
   });
   for_each<NB - 1>([&](auto T) MX_INLINE {
     constexpr int t = decltype(T)::value;
-    for_each<kLoads>([&](auto K) MX_INLINE { issue(K, t, t, (t + 1) / 2); });
+    begin_stage();
+    for_each<kLoads>([&](auto K) MX_INLINE { issue(K, t & 1, t, (t + 1) / 2); });
+    end_stage();
   });
-  for_each<LH::value>([&](auto K) MX_INLINE { issue(K, NB - 1, NB - 1, NB / 2); });
+  begin_stage();
+  for_each<LH::value>([&](auto K) MX_INLINE { issue(K, 0, NB - 1, NB / 2); });
   wait_vm<(NB - 2) * kLoads + LH::value>();
   wait_lds_and_meet();
   Half f0, f1;
-  for_each<kReads>([&](auto K) MX_INLINE { read(K, f0, 0, 0, 0, 0, 0); });
+  for_each<kReads + TM + TN>([&](auto K) MX_INLINE { read(K, f0, 0, 0, 0, 0, 0); });
   // lpair: the pair buffer of the loads for stage t + NB - 1; pair0, pair1: those of
   // stage t. A pair's buffer is taken up two stages later by the pair kPairs on.
   Place at{0, 0, 0, 0};
   int before = NB - 1, lpair = NB / 2;
   auto wrap = [](int v, int n) MX_INLINE { return v == n ? 0 : v; };
-  for (int t = 0; t < count; ++t) {
+  // Stores of whole tiles stay in flight over the first meeting of the next tile: at
+  // least that many operations are younger than the loads it waits for.
+  constexpr int kStores = sizeof(OutT) == 4 ? TM * TN * 16 : TM * TN * 8;
+  constexpr int kRelaxed = (NB - 2) * kLoads + kStores < 63 ? (NB - 2) * kLoads + kStores : 63;
+  bool relaxed = false;
+  while (true) {
+  for (int t = 0; t < now.count; ++t) {
     const int odd = t & 1;
     const Place next{t + 1, wrap(at.buf + 1, NB), wrap(at.pair0 + odd, kPairs),
                      wrap(at.pair1 + 1 - odd, kPairs)};
+#pragma unroll
+    for (int q = 0; q < TM + TN; ++q) scales[q] = words[q] >> (8 * hi);
     __builtin_amdgcn_sched_barrier(0);
-    half(f0, H0{}, f1, at, 1, LH{}, LN{}, t + NB - 1, before, lpair);
-    wait_vm<(NB - 2) * kLoads>();
+    half(f0, H0{}, f1, at, 1, LH{}, LN{}, odd, before, lpair);
+    if (relaxed) {
+      wait_vm<kRelaxed>();
+      relaxed = false;
+    } else {
+      wait_vm<(NB - 2) * kLoads>();
+    }
+    end_stage();
+    begin_stage();
     wait_lds_and_meet();
     __builtin_amdgcn_sched_barrier(0);
     // (stage t + NB's columns' half is that of stage t + 1: its last pair has ended)
     const int freed = odd ? at.pair0 : at.pair1;
-    half(f1, H1{}, f0, next, 0, L0{}, LH{}, t + NB, at.buf, freed);
+    half(f1, H1{}, f0, next, 0, L0{}, LH{}, 1 - odd, at.buf, freed);
     before = at.buf;
     lpair = freed;
     at = next;
   }
-  wait_vm<0>();
+  at.stage = 0;
 
   // ---- outputs: register i holds row i % 4 + 8 (i / 4) + 4 hi, column r32 ----
   const bool partial = a.splits > 1;
-  const int64_t bw = m0 + wm * TM * 32, ow = n0 + wn * TN * 32;
+  const int64_t bw = int64_t(now.mt) * BM + wm * TM * 32, ow = int64_t(now.nt) * BN + wn * TN * 32;
   const int brows = int(min(a.batch - bw, int64_t(BM))) - 4 * hi;
   const int ocols = int(min(a.out - ow, int64_t(BN))) - r32;
   const bool full = a.batch - bw >= TM * 32 && a.out - ow >= TN * 32;
   if (sizeof(OutT) == 4 || partial) {
-    float* const y = static_cast<float*>(a.y) + (partial ? split * a.batch * a.out : 0) +
+    float* const y = static_cast<float*>(a.y) + (partial ? now.split * a.batch * a.out : 0) +
                      bw * a.out + ow;
     const uint32_t lane_at = uint32_t(4 * hi) * uint32_t(a.out) + uint32_t(r32);
 #pragma unroll
@@ -377,6 +444,15 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
         }
       }
   }
+  if (now.item + step >= end) break;
+  now = locate(now.item + step);
+  relaxed = full;
+#pragma unroll
+  for (int m = 0; m < TM; ++m)
+#pragma unroll
+    for (int n = 0; n < TN; ++n) acc[m][n] = f32x16{};
+  }
+  wait_vm<0>();
 }
 
 // Sums of the splits in their order, four outputs at a time.
@@ -433,7 +509,7 @@ Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt, int g) {
   Plan p{};
   p.shape = batch <= kDecodeRows ? -1 : 0;
   p.splits = 1;
-  p.stages = (in + 127) / 128;
+  p.stages = (in + 255) / 256 * 2;
   p.rows32 = (batch + 31) / 32 * 32;
   p.x_bytes = up256(p.rows32 / 32 * p.stages * 2 * mx_half_bytes(fmt));
   p.xs_bytes = up256(p.rows32 * p.stages * 4);
@@ -449,7 +525,7 @@ Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt, int g) {
 template <int BM, int BN, int WM, int WN, int NB, int PERCU, int FMT, typename OutT>
 hipError_t launch_tiles(const Args& a, hipStream_t stream) {
   hipLaunchKernelGGL((mx_product_tiles<BM, BN, WM, WN, NB, PERCU, FMT, OutT>),
-                     dim3(unsigned(a.mtiles) * unsigned(a.ntiles) * unsigned(a.splits)),
+                     dim3(unsigned(std::min(a.mtiles * a.ntiles * a.splits, 256 * PERCU))),
                      dim3(64 * WM * WN), 0, stream, a);
   return hipGetLastError();
 }
