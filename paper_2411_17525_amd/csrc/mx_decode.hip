@@ -299,8 +299,11 @@ hipError_t launch(const Args& a, hipStream_t stream) {
   // as few waves as take equal shares of the chunks in as many turns as the most would
   const int turns = (a.chunks + kMaxWaves - 1) / kMaxWaves;
   const int waves = (a.chunks + turns - 1) / turns;
-  // one block per compute unit, or fewer
-  hipLaunchKernelGGL((mx_decode<FMT, G, NT>), dim3(unsigned(std::min(a.tiles, 256))),
+  // as many blocks as the compute units hold, or fewer: two each, one where the
+  // activations are in LDS too or with two tiles of them (16 x 4096 -> 28672 with 256
+  // blocks instead of 512: 21.3 us, not 18.7)
+  constexpr int kBlocks = G < 0 && NT == 1 ? 512 : 256;
+  hipLaunchKernelGGL((mx_decode<FMT, G, NT>), dim3(unsigned(std::min(a.tiles, kBlocks))),
                      dim3(unsigned(64 * waves)), 0, stream, a);
   return hipGetLastError();
 }

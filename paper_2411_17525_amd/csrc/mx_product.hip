@@ -521,13 +521,14 @@ double plan_us(const Shape& s, int splits, int64_t batch, int64_t out, int64_t i
   return t;
 }
 
-// Up to kStreamRows rows the weights are streamed (mx_decode). With more than 16 of
-// them only where the tile product would have to split K to fill the chip, below 80
-// blocks of 128 outputs (20 x 4096 -> 4096: 8.9 us against 12.7; -> 28672: 23.0
-// against 21.5).
+// Up to 16 rows the weights are streamed (mx_decode); up to 32 where that is faster: a
+// block's share of the tiles of 16 outputs times a wave's share of the chunks, 2.4 us
+// each, against the tile product with its scale words (20 x 4096 -> 4096: 8.9 us
+// against 12.7; 20 x 13824 -> 5120: 25.1 against 20.3).
 constexpr int64_t kStreamRows = 32;
-bool streams(int64_t batch, int64_t out) {
-  return batch <= 16 || (batch <= kStreamRows && out <= 80 * 128);
+double stream_us(int64_t out, int64_t in) {
+  const int64_t tiles = (out + 15) / 16, chunks = (in + 511) / 512;
+  return 1.6 + 2.4 * double((tiles + kCus - 1) / kCus) * double((chunks + 7) / 8);
 }
 
 // A call's shape, splits and workspace: activation codes and scales, weight scale
@@ -545,20 +546,23 @@ Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt, int g) {
   p.rows32 = (batch + 31) / 32 * 32;
   p.x_bytes = up256(p.rows32 / 32 * p.stages * 2 * mx_half_bytes(fmt));
   p.xs_bytes = up256(p.rows32 * p.stages * 4);
-  if (streams(batch, out)) {
+  double best = 0.0;
+  if (batch > 16) {
+    if (batch <= kStreamRows) best = stream_us(out, in) - double(out) * double(in) * 0.052e-6;
+    for (int s = 0; s < kNumShapes; ++s)
+      for (int k = 1; k <= 8 && k <= p.stages / 2; ++k) {
+        const double t = plan_us(kShapes[s], k, batch, out, in, p.stages);
+        if ((p.shape < 0 && batch > kStreamRows) || t < best) {
+          best = t;
+          p.shape = s;
+          p.splits = k;
+        }
+      }
+  }
+  if (p.shape < 0) {
     if (mx_decode_fuses(batch, in, g)) p.x_bytes = p.xs_bytes = 0;
     return p;
   }
-  double best = 0.0;
-  for (int s = 0; s < kNumShapes; ++s)
-    for (int k = 1; k <= 8 && k <= p.stages / 2; ++k) {
-      const double t = plan_us(kShapes[s], k, batch, out, in, p.stages);
-      if (p.shape < 0 || t < best) {
-        best = t;
-        p.shape = s;
-        p.splits = k;
-      }
-    }
   p.ws_bytes = up256(out * p.stages * 4);
   p.part_bytes = p.splits > 1 ? up256(p.splits * batch * out * 4) : 0;
   return p;
