@@ -28,9 +28,10 @@ typedef __attribute__((address_space(3))) void lds_void;
 struct Args {
   MxTiles x;
   const uint8_t* wc;
-  const uint32_t* ws;  // weight scales, a word per stage and row: [stage][out]
+  const uint32_t* ws;  // weight scales, a word per stage and row: [stage][pitch]
   void* y;             // or fp32 partial sums [split][batch][out]
   int64_t batch, out;
+  int64_t pitch;  // of a row of y and of ws, in values: out, or more for a part of the outputs
   int blocks;  // of a weight row
   int splits;  // of K
   int mtiles, ntiles;
@@ -154,10 +155,10 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
     const int nrows = int(min(int64_t(BN), a.out - n0));
     xp = a.x.codes + (m0 / 32 * stages + ltile.first) * kTile;
     xsp = a.x.scales + (ltile.first * a.x.rows32 + m0) * 4;
-    wsp = a.ws + ltile.first * a.out + n0;
+    wsp = a.ws + ltile.first * a.pitch + n0;
     xbytes = live ? uint32_t(((mrows / 32 - 1) * stages + ltile.count) * kTile) : 0;
     xsbytes = live ? uint32_t(((ltile.count - 1) * a.x.rows32 + mrows) * 4) : 0;
-    wsbytes = live ? uint32_t(((ltile.count - 1) * a.out + nrows) * 4) : 0;
+    wsbytes = live ? uint32_t(((ltile.count - 1) * a.pitch + nrows) * 4) : 0;
 #pragma unroll
     for (int i = 0; i < kXPer; ++i) {
       const int j = min(wave + i * kWaves, kXLoads - 1);
@@ -223,7 +224,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           rsrc(is_x ? static_cast<const void*>(xsp) : wsp, is_x ? xsbytes : wsbytes),
           (lds_void*)(s + kXScale + j * 256), 4, int(soff[i]), 0, 0, 0);
-      soff[i] += uint32_t(is_x ? a.x.rows32 : a.out) * 4;
+      soff[i] += uint32_t(is_x ? a.x.rows32 : a.pitch) * 4;
     } else {
       constexpr int i = k - kXPer - kSPer;
       const int j = wave + i * kWaves;
@@ -402,9 +403,9 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   const int ocols = int(min(a.out - ow, int64_t(BN))) - r32;
   const bool full = a.batch - bw >= TM * 32 && a.out - ow >= TN * 32;
   if (sizeof(OutT) == 4 || partial) {
-    float* const y = static_cast<float*>(a.y) + (partial ? now.split * a.batch * a.out : 0) +
-                     bw * a.out + ow;
-    const uint32_t lane_at = uint32_t(4 * hi) * uint32_t(a.out) + uint32_t(r32);
+    float* const y = static_cast<float*>(a.y) + (partial ? now.split * a.batch * a.pitch : 0) +
+                     bw * a.pitch + ow;
+    const uint32_t lane_at = uint32_t(4 * hi) * uint32_t(a.pitch) + uint32_t(r32);
 #pragma unroll
     for (int m = 0; m < TM; ++m)
 #pragma unroll
@@ -413,16 +414,16 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
 #pragma unroll
         for (int n = 0; n < TN; ++n)
           if (full || (b < brows && n * 32 < ocols))
-            y[b * a.out + n * 32 + lane_at] = acc[m][n][i];
+            y[b * a.pitch + n * 32 + lane_at] = acc[m][n][i];
       }
   } else {
     // two rows of a column per word; lanes 2 j and 2 j + 1 exchange them to two
     // columns of a row, lane 2 j storing the first row and lane 2 j + 1 the second
-    uint16_t* const y = static_cast<uint16_t*>(a.y) + bw * a.out + ow;
+    uint16_t* const y = static_cast<uint16_t*>(a.y) + bw * a.pitch + ow;
     const int odd = lane & 1;
-    const bool pairs = full && a.out % 2 == 0;
-    const uint32_t lane_at = uint32_t(4 * hi + odd) * uint32_t(a.out) + uint32_t(r32 - odd);
-    const uint32_t each_at = uint32_t(4 * hi) * uint32_t(a.out) + uint32_t(r32);
+    const bool pairs = full && a.pitch % 2 == 0;
+    const uint32_t lane_at = uint32_t(4 * hi + odd) * uint32_t(a.pitch) + uint32_t(r32 - odd);
+    const uint32_t each_at = uint32_t(4 * hi) * uint32_t(a.pitch) + uint32_t(r32);
 #pragma unroll
     for (int m = 0; m < TM; ++m)
 #pragma unroll
@@ -436,10 +437,10 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
             // even: (own low, partner's low); odd: (partner's high, own high)
             const uint32_t w = odd ? __builtin_amdgcn_perm(v, p, 0x07060302u)
                                    : __builtin_amdgcn_perm(p, v, 0x05040100u);
-            *reinterpret_cast<uint32_t*>(y + b * a.out + n * 32 + lane_at) = w;
+            *reinterpret_cast<uint32_t*>(y + b * a.pitch + n * 32 + lane_at) = w;
           } else if (n * 32 < ocols) {
-            if (b < brows) y[b * a.out + n * 32 + each_at] = uint16_t(v);
-            if (b + 1 < brows) y[(b + 1) * a.out + n * 32 + each_at] = uint16_t(v >> 16);
+            if (b < brows) y[b * a.pitch + n * 32 + each_at] = uint16_t(v);
+            if (b + 1 < brows) y[(b + 1) * a.pitch + n * 32 + each_at] = uint16_t(v >> 16);
           }
         }
       }
@@ -531,40 +532,67 @@ double stream_us(int64_t out, int64_t in) {
   return 1.6 + 2.4 * double((tiles + kCus - 1) / kCus) * double((chunks + 7) / 8);
 }
 
-// A call's shape, splits and workspace: activation codes and scales, weight scale
-// words, partial sums.
+struct Choice {
+  int shape, splits;
+  double us;
+};
+// The fastest shape and number of splits (up to max_splits) of a product.
+Choice best_of(int64_t batch, int64_t out, int64_t in, int64_t stages, int max_splits) {
+  Choice best{-1, 1, 0.0};
+  for (int s = 0; s < kNumShapes; ++s)
+    for (int k = 1; k <= max_splits && k <= stages / 2; ++k) {
+      const double t = plan_us(kShapes[s], k, batch, out, in, stages);
+      if (best.shape < 0 || t < best.us) best = Choice{s, k, t};
+    }
+  return best;
+}
+
+// A call's product, or two over parts of the outputs, and workspace: activation codes
+// and scales, weight scale words, partial sums.
 struct Plan {
-  int shape, splits;  // shape -1: mx_decode
+  Choice main;      // shape -1: mx_decode
+  Choice rest;      // of the outputs from `cut`, where that is below `out`
+  int64_t cut;
   int64_t stages, rows32, x_bytes, xs_bytes, ws_bytes, part_bytes;
   int64_t bytes() const { return x_bytes + xs_bytes + ws_bytes + part_bytes; }
 };
 Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt, int g) {
   Plan p{};
-  p.shape = -1;
-  p.splits = 1;
+  p.main = Choice{-1, 1, 0.0};
+  p.cut = out;
   p.stages = (in + 255) / 256 * 2;
   p.rows32 = (batch + 31) / 32 * 32;
   p.x_bytes = up256(p.rows32 / 32 * p.stages * 2 * mx_half_bytes(fmt));
   p.xs_bytes = up256(p.rows32 * p.stages * 4);
-  double best = 0.0;
   if (batch > 16) {
-    if (batch <= kStreamRows) best = stream_us(out, in) - double(out) * double(in) * 0.052e-6;
-    for (int s = 0; s < kNumShapes; ++s)
-      for (int k = 1; k <= 8 && k <= p.stages / 2; ++k) {
-        const double t = plan_us(kShapes[s], k, batch, out, in, p.stages);
-        if ((p.shape < 0 && batch > kStreamRows) || t < best) {
-          best = t;
-          p.shape = s;
-          p.splits = k;
-        }
-      }
+    const Choice c = best_of(batch, out, in, p.stages, 8);
+    if (batch > kStreamRows ||
+        c.us + double(out) * double(in) * 0.052e-6 < stream_us(out, in))
+      p.main = c;
   }
-  if (p.shape < 0) {
+  if (p.main.shape < 0) {
     if (mx_decode_fuses(batch, in, g)) p.x_bytes = p.xs_bytes = 0;
     return p;
   }
+  // Tiles that fill whole rounds of a shape as one product, the columns left over as
+  // another of smaller blocks instead of a round that leaves units idle (2048 x 4096 ->
+  // 28672: 3.5 rounds of 256 x 256; three and one of 128 x 256 take XX us, not 162).
+  for (const Shape& s : kShapes) {
+    const int64_t mt = (batch + s.bm - 1) / s.bm, nt = (out + s.bn - 1) / s.bn;
+    const int64_t rounds = mt * nt / (kCus * s.percu);
+    const int64_t cut = rounds * kCus * s.percu / mt * s.bn;
+    if (rounds < 1 || cut < 1 || cut >= out) continue;
+    const Choice first{int(&s - kShapes), 1, plan_us(s, 1, batch, cut, in, p.stages)};
+    const Choice rest = best_of(batch, out - cut, in, p.stages, 1);
+    // (and a launch's gap)
+    if (first.us + rest.us + 3.0 < p.main.us + (p.cut < out ? p.rest.us + 3.0 : 0.0)) {
+      p.main = first;
+      p.rest = rest;
+      p.cut = cut;
+    }
+  }
   p.ws_bytes = up256(out * p.stages * 4);
-  p.part_bytes = p.splits > 1 ? up256(p.splits * batch * out * 4) : 0;
+  p.part_bytes = p.main.splits > 1 ? up256(p.main.splits * batch * out * 4) : 0;
   return p;
 }
 
@@ -592,13 +620,22 @@ hipError_t launch_shape(int shape, Args a, hipStream_t stream) {
 template <int FMT, typename OutT>
 hipError_t launch_product(const Plan& p, const Args& args, float* part, hipStream_t stream) {
   Args a = args;
-  a.splits = p.splits;
-  if (p.splits > 1) a.y = part;
-  const hipError_t st = launch_shape<FMT, OutT>(p.shape, a, stream);
-  if (st != hipSuccess || p.splits == 1) return st;
+  a.splits = p.main.splits;
+  a.out = p.cut;
+  if (a.splits > 1) a.y = part;
+  hipError_t st = launch_shape<FMT, OutT>(p.main.shape, a, stream);
+  if (st != hipSuccess) return st;
+  if (p.cut < args.out) {
+    a.out = args.out - p.cut;
+    a.wc += p.cut * a.blocks * 16;
+    a.ws += p.cut;
+    a.y = static_cast<OutT*>(args.y) + p.cut;
+    return launch_shape<FMT, OutT>(p.rest.shape, a, stream);
+  }
+  if (a.splits == 1) return hipSuccess;
   const int64_t total = a.batch * a.out;
   hipLaunchKernelGGL((mx_sum_splits<OutT>), dim3(unsigned((total + 1023) / 1024)), dim3(256), 0,
-                     stream, part, p.splits, total, static_cast<OutT*>(args.y));
+                     stream, part, a.splits, total, static_cast<OutT*>(args.y));
   return hipGetLastError();
 }
 
@@ -624,7 +661,7 @@ hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, 
   if (p.x_bytes > 0)
     st = launch_mx_tiles(x, x_dtype, batch, in, fmt, g, seed, a.x, w_scales, stream);
   if (st != hipSuccess) return st;
-  if (p.shape < 0)
+  if (p.main.shape < 0)
     return launch_mx_decode(x, x_dtype, batch, fmt, a.x, codes, scales, g, seed, out, in, y, y_dtype,
                             stream);
   a.wc = codes;
@@ -632,6 +669,7 @@ hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, 
   a.y = y;
   a.batch = batch;
   a.out = out;
+  a.pitch = out;
   a.blocks = int(mx_blocks(in));
   if (fmt == HIGGS_MX_FP4)
     return y_dtype == HIGGS_F32 ? launch_product<HIGGS_MX_FP4, float>(p, a, part, stream)
