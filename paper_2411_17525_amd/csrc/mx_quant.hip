@@ -320,14 +320,26 @@ __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__
 
 // ---- the way back ----
 
-// Rotated back in fp32 (stored values are not decided at borders): 16 consecutive
-// values per lane throughout, butterflies over lanes by DPP and permlane, no LDS.
+// Rotated back in fp32 (stored values are not decided at borders). Groups of 1024
+// through LDS (fwht1024_lds: 260 vector instructions per segment instead of 450, 39
+// instead of 52 us for 4096 x 14336 to bf16), which leaves four runs of four
+// consecutive values per lane; smaller groups in place, by DPP and permlane.
 template <int G, int FMT, typename OutT>
 __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht(
     const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t total,
     const MxSigns signs, float root, OutT* __restrict__ w) {
+  constexpr bool kLds = G == 1024;
+  __shared__ __attribute__((aligned(16))) float s_lds[kLds ? kWaves : 1][kLds ? kFwht1024Scratch : 4];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  const uint32_t neg = lane_signs<G>(signs, lane);
+  // signs of the values that the lane ends with
+  uint32_t neg = 0;
+  if constexpr (kLds) {
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      neg |= ((signs.w[8 * h + (lane >> 3)] >> (4 * lane & 31)) & 15) << (4 * h);
+  } else {
+    neg = lane_signs<G>(signs, lane);
+  }
   const int64_t segs = (total + 1023) / 1024, step = int64_t(gridDim.x) * kWaves;
   for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
     const int64_t at = 1024 * seg + 16 * lane;
@@ -337,15 +349,32 @@ __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht(
       load_codes16<FMT>(codes + (at / 16) * (4 * kWords16<FMT>), c);
       byte = scales[at / 32];
     }
-    float x[16];
+    float x[16], s = root;
     mx_decode16<FMT>(c, byte, x);
-    fwht_in_lane<16>(x);
-    const float s = fwht_cross_lane_deferred_fixed<16, G>(x, lane) * root;
+    if constexpr (kLds) {
+      fwht1024_lds(x, s_lds[wave], lane);
+    } else {
+      fwht_in_lane<16>(x);
+      s *= fwht_cross_lane_deferred_fixed<16, G>(x, lane);
+    }
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       x[i] = __builtin_bit_cast(
           float, __builtin_bit_cast(uint32_t, x[i] * s) ^ ((neg << (31 - i)) & 0x80000000u));
-    if (live) store16(w + at, x);
+    if constexpr (kLds) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        OutT* const p = w + 1024 * seg + 256 * h + 4 * lane;
+        if constexpr (sizeof(OutT) == 2)
+          *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x[4 * h], x[4 * h + 1]),
+                                                    pack_bf16(x[4 * h + 2], x[4 * h + 3]));
+        else
+          *reinterpret_cast<float4*>(p) =
+              make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
+      }
+    } else if (live) {
+      store16(w + at, x);
+    }
   }
 }
 
