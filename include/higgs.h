@@ -527,7 +527,7 @@ higgs_status higgs_mx_dequantize(const uint8_t *codes, const uint8_t *scales, in
  *   t2       [out] device, nullable, one double: the ratio of their totals (0
  *            for an all-zero layer).
  * Other arguments as for higgs_mx_quantize. W must hold finite values (others
- * make the row's error and t2 NaN or infinite). Requires out < 2^31. */
+ * make the row's error and t2 NaN or infinite). Requires out < 2^24. */
 higgs_status higgs_mx_layer_error(const void *W, higgs_dtype w_dtype, int64_t out, int64_t in,
                                   const uint8_t *codes, const uint8_t *scales, int g,
                                   uint64_t rht_seed, double *row_err, double *t2, void *stream);
@@ -548,8 +548,9 @@ higgs_status higgs_mx_layer_error(const void *W, higgs_dtype w_dtype, int64_t ou
  *                    higgs_mx_qmatmul_workspace_bytes(...) bytes, 256-byte
  *                    aligned (may be NULL when that is 0); not preserved. Calls
  *                    that overlap in time need workspaces of their own.
- * Requires batch >= 1, out >= 1, in >= 1, batch * in <= 2^36, batch * out <=
- * 2^40, in <= 2^20, codes below 2 GiB (HIGGS_ERR_UNSUPPORTED otherwise). */
+ * Requires batch >= 1, out >= 1, in >= 1; in <= 2^20, batch and out below 2^24,
+ * batch * in <= 2^34, batch * out <= 2^38, codes below 2 GiB
+ * (HIGGS_ERR_UNSUPPORTED otherwise). */
 int64_t higgs_mx_qmatmul_workspace_bytes(int64_t batch, int64_t out, int64_t in,
                                          higgs_mx_format x_fmt, int g);
 higgs_status higgs_mx_qmatmul(const void *x, higgs_dtype x_dtype, int64_t batch,

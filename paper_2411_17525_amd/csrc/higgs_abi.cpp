@@ -518,6 +518,9 @@ higgs_status higgs_qmatmul_fused_multi(int layers, const void* x, higgs_dtype x_
 
 namespace {
 
+// Rows that have a block of their own in a launch (2^32 threads at most).
+constexpr int64_t kMxMaxRows = int64_t(1) << 24;
+
 // Shared checks of the microscaled entry points.
 higgs_status check_mx(higgs_dtype dtype, const char* dtype_name, int64_t rows, int64_t in, int fmt,
                       int g) {
@@ -538,7 +541,7 @@ higgs_status check_mx(higgs_dtype dtype, const char* dtype_name, int64_t rows, i
                   g);
   }
   if (rows > (int64_t(1) << 40) / in)
-    return fail(HIGGS_ERR_UNSUPPORTED, "rows * in must be below 2^40");
+    return fail(HIGGS_ERR_UNSUPPORTED, "rows * in must be at most 2^40");
   return HIGGS_OK;
 }
 
@@ -551,10 +554,12 @@ higgs_status check_mx_product(int64_t batch, int64_t out, int64_t in, int fmt, i
   // the kernels address codes with 32-bit byte offsets
   if (out * higgs::mx_blocks(in) * 16 >= (int64_t(1) << 31))
     return fail(HIGGS_ERR_UNSUPPORTED, "layer too large: codes must be < 2 GiB");
-  if (batch > (int64_t(1) << 36) / in)
-    return fail(HIGGS_ERR_UNSUPPORTED, "batch * in must be below 2^36");
-  if (batch > (int64_t(1) << 40) / out)
-    return fail(HIGGS_ERR_UNSUPPORTED, "batch * out must be below 2^40");
+  if (batch >= kMxMaxRows || out >= kMxMaxRows)
+    return fail(HIGGS_ERR_UNSUPPORTED, "batch and out must be below 2^24");
+  if (batch > (int64_t(1) << 34) / in)
+    return fail(HIGGS_ERR_UNSUPPORTED, "batch * in must be at most 2^34");
+  if (batch > (int64_t(1) << 38) / out)
+    return fail(HIGGS_ERR_UNSUPPORTED, "batch * out must be at most 2^38");
   return HIGGS_OK;
 }
 
@@ -607,8 +612,8 @@ higgs_status higgs_mx_layer_error(const void* W, higgs_dtype w_dtype, int64_t ou
     return fail(HIGGS_ERR_INVALID_ARG, "W, codes, scales and row_err must not be NULL");
   const higgs_status st = check_mx(w_dtype, "w_dtype", out, in, HIGGS_MX_FP4, g);
   if (st != HIGGS_OK) return st;
-  if (out >= (int64_t(1) << 31))
-    return fail(HIGGS_ERR_UNSUPPORTED, "out (%lld) must be below 2^31", (long long)out);
+  if (out >= kMxMaxRows)
+    return fail(HIGGS_ERR_UNSUPPORTED, "out (%lld) must be below 2^24", (long long)out);
   if (!aligned(W, 16) || !aligned(codes, 16) || !aligned(row_err, 8) || !aligned(t2, 8))
     return fail(HIGGS_ERR_INVALID_ARG,
                 "W and codes must be 16-byte aligned, row_err and t2 8");

@@ -53,7 +53,7 @@ __host__ __device__ inline int64_t mx_tile_unit(const MxTiles& t, uint32_t row, 
 hipError_t launch_mx_quantize(const void* w, higgs_dtype dtype, int64_t rows, int64_t in, int fmt,
                               int g, uint64_t seed, uint8_t* codes, uint8_t* scales,
                               hipStream_t stream);
-// Activations into the product's order (batch * in <= 2^36) and, in the same launch,
+// Activations into the product's order (batch * in <= 2^34) and, in the same launch,
 // weight scale words (none where words.to is NULL).
 hipError_t launch_mx_tiles(const void* x, higgs_dtype dtype, int64_t batch, int64_t in, int fmt,
                            int g, uint64_t seed, const MxTiles& tiles, const MxScaleWords& words,

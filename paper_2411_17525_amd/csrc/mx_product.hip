@@ -62,9 +62,9 @@ __device__ MX_INLINE inline void for_each(const F& f) {
 }
 
 // A block computes tiles of BM activation rows x BN outputs over a range of K with
-// WM x WN waves, one after another, stage by stage of 128 values: the stage's activations, weights and scale
-// words go from memory to LDS, from there into the operands. The loads run NB - 1/2
-// stages ahead. Weights are loaded for two stages at a time, 128 bytes of a
+// WM x WN waves, one after another, stage by stage of 128 values: the stage's
+// activations, weights and scale words go from memory to LDS, from there into the
+// operands. The loads run NB - 1/2 stages ahead. Weights are loaded for two stages at a time, 128 bytes of a
 // row: the address unit takes about as long for half a line as for a whole one
 // (62, 88 and 106 GB/s per compute unit in pieces of 64, 128 and 256 bytes), and
 // that time is what the products have to hide. So that every stage loads as much,
@@ -369,89 +369,89 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   constexpr int kRelaxed = (NB - 2) * kLoads + kStores < 63 ? (NB - 2) * kLoads + kStores : 63;
   bool relaxed = false;
   while (true) {
-  for (int t = 0; t < now.count; ++t) {
-    const int odd = t & 1;
-    const Place next{t + 1, wrap(at.buf + 1, NB), wrap(at.pair0 + odd, kPairs),
-                     wrap(at.pair1 + 1 - odd, kPairs)};
+    for (int t = 0; t < now.count; ++t) {
+      const int odd = t & 1;
+      const Place next{t + 1, wrap(at.buf + 1, NB), wrap(at.pair0 + odd, kPairs),
+                       wrap(at.pair1 + 1 - odd, kPairs)};
 #pragma unroll
-    for (int q = 0; q < TM + TN; ++q) scales[q] = words[q] >> (8 * hi);
-    __builtin_amdgcn_sched_barrier(0);
-    half(f0, H0{}, f1, at, 1, LH{}, LN{}, odd, before, lpair);
-    if (relaxed) {
-      wait_vm<kRelaxed>();
-      relaxed = false;
-    } else {
-      wait_vm<(NB - 2) * kLoads>();
-    }
-    end_stage();
-    begin_stage();
-    wait_lds_and_meet();
-    __builtin_amdgcn_sched_barrier(0);
-    // (stage t + NB's columns' half is that of stage t + 1: its last pair has ended)
-    const int freed = odd ? at.pair0 : at.pair1;
-    half(f1, H1{}, f0, next, 0, L0{}, LH{}, 1 - odd, at.buf, freed);
-    before = at.buf;
-    lpair = freed;
-    at = next;
-  }
-  at.stage = 0;
-
-  // ---- outputs: register i holds row i % 4 + 8 (i / 4) + 4 hi, column r32 ----
-  const bool partial = a.splits > 1;
-  const int64_t bw = int64_t(now.mt) * BM + wm * TM * 32, ow = int64_t(now.nt) * BN + wn * TN * 32;
-  const int brows = int(min(a.batch - bw, int64_t(BM))) - 4 * hi;
-  const int ocols = int(min(a.out - ow, int64_t(BN))) - r32;
-  const bool full = a.batch - bw >= TM * 32 && a.out - ow >= TN * 32;
-  if (sizeof(OutT) == 4 || partial) {
-    float* const y = static_cast<float*>(a.y) + (partial ? now.split * a.batch * a.pitch : 0) +
-                     bw * a.pitch + ow;
-    const uint32_t lane_at = uint32_t(4 * hi) * uint32_t(a.pitch) + uint32_t(r32);
-#pragma unroll
-    for (int m = 0; m < TM; ++m)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int b = m * 32 + i % 4 + 8 * (i / 4);
-#pragma unroll
-        for (int n = 0; n < TN; ++n)
-          if (full || (b < brows && n * 32 < ocols))
-            y[b * a.pitch + n * 32 + lane_at] = acc[m][n][i];
+      for (int q = 0; q < TM + TN; ++q) scales[q] = words[q] >> (8 * hi);
+      __builtin_amdgcn_sched_barrier(0);
+      half(f0, H0{}, f1, at, 1, LH{}, LN{}, odd, before, lpair);
+      if (relaxed) {
+        wait_vm<kRelaxed>();
+        relaxed = false;
+      } else {
+        wait_vm<(NB - 2) * kLoads>();
       }
-  } else {
-    // two rows of a column per word; lanes 2 j and 2 j + 1 exchange them to two
-    // columns of a row, lane 2 j storing the first row and lane 2 j + 1 the second
-    uint16_t* const y = static_cast<uint16_t*>(a.y) + bw * a.pitch + ow;
-    const int odd = lane & 1;
-    const bool pairs = full && a.pitch % 2 == 0;
-    const uint32_t lane_at = uint32_t(4 * hi + odd) * uint32_t(a.pitch) + uint32_t(r32 - odd);
-    const uint32_t each_at = uint32_t(4 * hi) * uint32_t(a.pitch) + uint32_t(r32);
+      end_stage();
+      begin_stage();
+      wait_lds_and_meet();
+      __builtin_amdgcn_sched_barrier(0);
+      // (stage t + NB's columns' half is that of stage t + 1: its last pair has ended)
+      const int freed = odd ? at.pair0 : at.pair1;
+      half(f1, H1{}, f0, next, 0, L0{}, LH{}, 1 - odd, at.buf, freed);
+      before = at.buf;
+      lpair = freed;
+      at = next;
+    }
+    at.stage = 0;
+
+    // ---- outputs: register i holds row i % 4 + 8 (i / 4) + 4 hi, column r32 ----
+    const bool partial = a.splits > 1;
+    const int64_t bw = int64_t(now.mt) * BM + wm * TM * 32, ow = int64_t(now.nt) * BN + wn * TN * 32;
+    const int brows = int(min(a.batch - bw, int64_t(BM))) - 4 * hi;
+    const int ocols = int(min(a.out - ow, int64_t(BN))) - r32;
+    const bool full = a.batch - bw >= TM * 32 && a.out - ow >= TN * 32;
+    if (sizeof(OutT) == 4 || partial) {
+      float* const y = static_cast<float*>(a.y) + (partial ? now.split * a.batch * a.pitch : 0) +
+                       bw * a.pitch + ow;
+      const uint32_t lane_at = uint32_t(4 * hi) * uint32_t(a.pitch) + uint32_t(r32);
 #pragma unroll
-    for (int m = 0; m < TM; ++m)
+      for (int m = 0; m < TM; ++m)
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const int b = m * 32 + i % 4 + 8 * (i / 4);
+        for (int i = 0; i < 16; ++i) {
+          const int b = m * 32 + i % 4 + 8 * (i / 4);
 #pragma unroll
-        for (int n = 0; n < TN; ++n) {
-          const uint32_t v = pack_bf16(acc[m][n][i], acc[m][n][i + 1]);
-          if (pairs) {
-            const uint32_t p = lane_xor_small<1>(v);
-            // even: (own low, partner's low); odd: (partner's high, own high)
-            const uint32_t w = odd ? __builtin_amdgcn_perm(v, p, 0x07060302u)
-                                   : __builtin_amdgcn_perm(p, v, 0x05040100u);
-            *reinterpret_cast<uint32_t*>(y + b * a.pitch + n * 32 + lane_at) = w;
-          } else if (n * 32 < ocols) {
-            if (b < brows) y[b * a.pitch + n * 32 + each_at] = uint16_t(v);
-            if (b + 1 < brows) y[(b + 1) * a.pitch + n * 32 + each_at] = uint16_t(v >> 16);
+          for (int n = 0; n < TN; ++n)
+            if (full || (b < brows && n * 32 < ocols))
+              y[b * a.pitch + n * 32 + lane_at] = acc[m][n][i];
+        }
+    } else {
+      // two rows of a column per word; lanes 2 j and 2 j + 1 exchange them to two
+      // columns of a row, lane 2 j storing the first row and lane 2 j + 1 the second
+      uint16_t* const y = static_cast<uint16_t*>(a.y) + bw * a.pitch + ow;
+      const int odd = lane & 1;
+      const bool pairs = full && a.pitch % 2 == 0;
+      const uint32_t lane_at = uint32_t(4 * hi + odd) * uint32_t(a.pitch) + uint32_t(r32 - odd);
+      const uint32_t each_at = uint32_t(4 * hi) * uint32_t(a.pitch) + uint32_t(r32);
+#pragma unroll
+      for (int m = 0; m < TM; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+          const int b = m * 32 + i % 4 + 8 * (i / 4);
+#pragma unroll
+          for (int n = 0; n < TN; ++n) {
+            const uint32_t v = pack_bf16(acc[m][n][i], acc[m][n][i + 1]);
+            if (pairs) {
+              const uint32_t p = lane_xor_small<1>(v);
+              // even: (own low, partner's low); odd: (partner's high, own high)
+              const uint32_t w = odd ? __builtin_amdgcn_perm(v, p, 0x07060302u)
+                                     : __builtin_amdgcn_perm(p, v, 0x05040100u);
+              *reinterpret_cast<uint32_t*>(y + b * a.pitch + n * 32 + lane_at) = w;
+            } else if (n * 32 < ocols) {
+              if (b < brows) y[b * a.pitch + n * 32 + each_at] = uint16_t(v);
+              if (b + 1 < brows) y[(b + 1) * a.pitch + n * 32 + each_at] = uint16_t(v >> 16);
+            }
           }
         }
-      }
-  }
-  if (now.item + step >= end) break;
-  now = locate(now.item + step);
-  relaxed = full;
+    }
+    if (now.item + step >= end) break;
+    now = locate(now.item + step);
+    relaxed = full;
 #pragma unroll
-  for (int m = 0; m < TM; ++m)
+    for (int m = 0; m < TM; ++m)
 #pragma unroll
-    for (int n = 0; n < TN; ++n) acc[m][n] = f32x16{};
+      for (int n = 0; n < TN; ++n) acc[m][n] = f32x16{};
   }
   wait_vm<0>();
 }
@@ -505,7 +505,6 @@ constexpr Shape kShapes[] = {{256, 256, 1, 0.54, 0.82, 5.7},
                              {64, 128, 2, 0.37, 0.28, 2.6},
                              {32, 128, 2, 0.26, 0.25, 1.9},
                              {128, 256, 1, 0.13, 0.57, 4.2}};
-constexpr int kNumShapes = int(sizeof(kShapes) / sizeof(kShapes[0]));
 constexpr int64_t kCus = 256;
 
 double plan_us(const Shape& s, int splits, int64_t batch, int64_t out, int64_t in,
@@ -539,10 +538,10 @@ struct Choice {
 // The fastest shape and number of splits (up to max_splits) of a product.
 Choice best_of(int64_t batch, int64_t out, int64_t in, int64_t stages, int max_splits) {
   Choice best{-1, 1, 0.0};
-  for (int s = 0; s < kNumShapes; ++s)
+  for (const Shape& s : kShapes)
     for (int k = 1; k <= max_splits && k <= stages / 2; ++k) {
-      const double t = plan_us(kShapes[s], k, batch, out, in, stages);
-      if (best.shape < 0 || t < best.us) best = Choice{s, k, t};
+      const double t = plan_us(s, k, batch, out, in, stages);
+      if (best.shape < 0 || t < best.us) best = Choice{int(&s - kShapes), k, t};
     }
   return best;
 }
@@ -576,7 +575,7 @@ Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt, int g) {
   }
   // Tiles that fill whole rounds of a shape as one product, the columns left over as
   // another of smaller blocks instead of a round that leaves units idle (2048 x 4096 ->
-  // 28672: 3.5 rounds of 256 x 256; three and one of 128 x 256 take XX us, not 162).
+  // 28672: 3.5 rounds of 256 x 256; three, and one of 128 x 256, take 154 us, not 162).
   for (const Shape& s : kShapes) {
     const int64_t mt = (batch + s.bm - 1) / s.bm, nt = (out + s.bn - 1) / s.bn;
     const int64_t rounds = mt * nt / (kCus * s.percu);

@@ -111,3 +111,21 @@ def test_binding_refuses_host_tensors():
                  lambda: H.mx_qmatmul(w, c, s, FP6, 0, 0, 4)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_limits_of_the_product(L):  # noqa: F811
+    """Counts that the kernels hold in 32 bits: the largest calls taken, the next refused."""
+    def need(batch, out, inp):
+        return H.mx_qmatmul_workspace_bytes(batch, out, inp, FP6, 0)
+    top = (1 << 24) - 1
+    assert need(top, 1, 32) > 0 and need(top + 1, 1, 32) == -1
+    assert need(40, top, 64) > 0 and need(40, top + 1, 64) == -1
+    assert need(1 << 14, 16, 1 << 20) > 0 and need((1 << 14) + 1, 16, 1 << 20) == -1
+    assert need(1 << 19, 1 << 19, 32) > 0 and need((1 << 19) + 1, 1 << 19, 32) == -1
+    assert need(40, (1 << 20) - 1, 4096) > 0 and need(40, 1 << 20, 4096) == -1
+
+
+@no_gpu
+def test_layer_error_refuses_more_rows_than_a_launch_holds(L):  # noqa: F811
+    assert L.higgs_mx_layer_error(FAKE, 1, 1 << 24, 64, FAKE, FAKE, 0, 0, FAKE, None,
+                                  None) == UNSUPPORTED
