@@ -16,8 +16,9 @@ constexpr int kMxTop = 2;
 inline int mx_block_bytes(int fmt) { return fmt == HIGGS_MX_FP4 ? 16 : 24; }
 inline int64_t mx_blocks(int64_t in) { return (in + kMxBlock - 1) / kMxBlock; }
 
-// RHT signs of a group of up to 4096: bit j % 32 of word j / 32 set iff
-// sigma_j = -1. A kernel argument: the kernels read it like any other.
+// RHT signs, a bit set where sigma_j = -1: of a group of 2048 or 4096 bit j % 32 of word
+// j / 32; of smaller ones as the lanes hold a segment of 1024 values (bits r and 16 + r of
+// word l: values 128 r + 2 l and 128 r + 2 l + 1). A kernel argument.
 struct MxSigns {
   uint32_t w[128];
 };

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
   // LDS: the waves' slots, the last of them the rotation's scratch first; two tiles'
   // partial sums; FUSED: the activations (16- and 8-byte parts, scale words)
   constexpr int kWaveRing =
-      (kRingSlots - 1) * kSlot + (G > 0 ? std::max(kSlot, kMxWaveLds * 4) : kSlot);
+      (kRingSlots - 1) * kSlot + (G > 0 ? std::max(kSlot, kMxWaveLds<double> * 4) : kSlot);
   constexpr int kRing = kMaxWaves * kWaveRing, kPart = kMaxWaves * NT * 16 * 16 * 4;
   constexpr int kXBlocks = kFused ? kFusedValues / 32 + 16 * 16 : 0;  // (whole stages per row)
   constexpr int kX = kRing + 2 * kPart, kXTail = kX + kXBlocks * 16;
@@ -160,37 +160,38 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
     auto put_scale = [&](int b, int kb, uint32_t byte) {
       s_mem[kXScale + ((kb >> 2) * batch + b) * 4 + (kb & 3)] = uint8_t(byte);
     };
-    auto load = [&](int b, int k, float (&x)[16]) {
-      const int left = a.in - k, n = left < 0 ? 0 : left > 16 ? 16 : left;
-      const int64_t at = int64_t(b) * a.in + (left > 0 ? k : 0);
-      if (a.x_bf16)
-        load16_upto(static_cast<const uint16_t*>(a.x) + at, n, x);
-      else
-        load16_upto(static_cast<const float*>(a.x) + at, n, x);
-    };
     if constexpr (G > 0) {
       uint32_t* const lds = reinterpret_cast<uint32_t*>(ring + (kRingSlots - 1) * kSlot);
-      const uint32_t neg = lane_signs<G>(a.signs, lane);
+      const MxPairSigns neg = pair_signs(a.signs, lane);
       const int segs = (a.in + 1023) / 1024;  // of a row; the last may end early
       for (int i = wave; i < batch * segs; i += waves) {
         const int b = i / segs, seg = i - b * segs;
-        float x[16];
-        load(b, 1024 * seg + 16 * lane, x);
+        const int64_t at = int64_t(b) * a.in + 1024 * seg;
+        double v[16];
+        if (a.x_bf16)
+          signed_pairs(load_pairs(static_cast<const uint16_t*>(a.x) + at, a.in - 1024 * seg, lane), neg, v);
+        else
+          signed_pairs(load_pairs(static_cast<const float*>(a.x) + at, a.in - 1024 * seg, lane), neg, v);
         uint32_t c[kWords16<FMT>], byte;
-        int block;
-        mx_rotate_segment<G, FMT>(x, neg, a.root, lds, lane, c, &byte, &block);
+        mx_rotate_segment<G, FMT>(v, a.root, lds, lane, c, &byte);
         // (up to the end of the row's last stage: zeros behind its values)
         const int half = 64 * seg + lane;
-        if (half < 8 * a.stages) put(b, half, c);
-        const int kb = 32 * seg + block;
-        if ((lane & 15) < 8 && kb < 4 * a.stages) put_scale(b, kb, byte);
+        if (half < 8 * a.stages) {
+          put(b, half, c);
+          if ((lane & 1) == 0) put_scale(b, half >> 1, byte);
+        }
       }
     } else {
       const int units = 8 * a.stages;
       for (int u = tid; u < batch * units; u += 64 * waves) {
         const int b = u / units, half = u - b * units;
+        const int left = a.in - 16 * half, n = left < 0 ? 0 : left > 16 ? 16 : left;
+        const int64_t at = int64_t(b) * a.in + (left > 0 ? 16 * half : 0);
         float x[16];
-        load(b, 16 * half, x);
+        if (a.x_bf16)
+          load16_upto(static_cast<const uint16_t*>(a.x) + at, n, x);
+        else
+          load16_upto(static_cast<const float*>(a.x) + at, n, x);
         uint32_t c[kWords16<FMT>];
         const uint32_t byte = mx_plain_halves<FMT>(x, c);
         put(b, half, c);

@@ -7,57 +7,89 @@
 
 namespace higgs {
 
-// LDS dwords per wave for a rotation: 1024 fp64 values.
-constexpr int kMxWaveLds = 2048;
+// Rotation of a segment of 1024 values by a wave, 16 per lane, groups of G (64 ..
+// 1024). With n = 512 .. 1 for the bits 9 .. 0 of a value's place, lane bits from low
+// to high, the values lie
+//   in pairs:  register bits 0, 7, 8, 9   lane bits 1 .. 6    v[2 r + b] is 128 r + 2 lane + b
+//   between:   register bits 0, 4, 5, 6   lane bits 1, 2, 3, 7, 8, 9
+//   in runs:   register bits 0 .. 3       lane bits 4 .. 9    v[i] is 16 lane + i
+// and go from one order to the next through LDS as pairs (16 bytes of fp64). Butterflies
+// are done over register bits only: in pairs those of 0, 7, 8, 9, between of 4, 5, 6, in
+// runs of 1, 2, 3. In pairs a load or store of the wave is one run of memory; in runs a
+// lane holds half a block: its largest, codes and scale take one step across lanes.
+// (With the values in runs first, 4 + 4 bits in registers, the last two by permlane
+// swaps and the way back to runs through LDS, a segment's quantization took 650
+// instructions, not 350.)
+template <typename T>
+constexpr int kMxWaveLds = 576 * 2 * int(sizeof(T)) / 4;  // dwords per wave
 
-// fwht_rows with whole values in LDS: the same sums in the same places from half the
-// LDS instructions and without moves that put the halves of a value together, for
-// twice the scratch (1024 values, 128-byte aligned).
-template <int G>
-__device__ inline void mx_fwht_rows(double (&v)[16], uint32_t* scratch, int lane) {
-  static_assert(G == 64 || G == 128 || G == 256 || G == 512 || G == 1024, "block size");
-  typedef double f64x2 __attribute__((ext_vector_type(2)));
-  wave_lds_sync();  // this wave's earlier accesses come first
-  fwht_in_lane<16>(v);
-  // value i of lane c of a row at 16 c + i, the pairs of a lane permuted by its low
-  // bits: eight lanes hit distinct banks
-  double* const row = reinterpret_cast<double*>(scratch) + 256 * (lane >> 4);
-  const int c = lane & 15;
+template <int H, typename T>
+__device__ inline void mx_butterflies(T (&v)[16]) {
 #pragma unroll
-  for (int p = 0; p < 8; ++p)
-    *reinterpret_cast<f64x2*>(row + 16 * c + 2 * (p ^ (c & 7))) = f64x2{v[2 * p], v[2 * p + 1]};
-  wave_lds_sync();
+  for (int i = 0; i < 16; ++i)
+    if ((i & H) == 0) {
+      const T x = v[i], y = v[i + H];
+      v[i] = x + y;
+      v[i + H] = x - y;
+    }
+}
+
+// H per group, from pairs to runs, or (BACK) from runs to pairs. Pair p is at p + 8 (p
+// / 64) of the scratch between pairs and the middle order, at p + p / 8 between that
+// and runs: both sides of both reach distinct banks.
+template <int G, bool BACK, typename T>
+__device__ inline void mx_fwht(T (&v)[16], uint32_t* scratch, int lane) {
+  static_assert(G == 64 || G == 128 || G == 256 || G == 512 || G == 1024, "group size");
+  typedef T pair_t __attribute__((ext_vector_type(2)));
+  pair_t* const pairs = reinterpret_cast<pair_t*>(scratch) + lane;
+  pair_t* const middle = reinterpret_cast<pair_t*>(scratch) + (lane & 7) + 72 * (lane >> 3);
+  pair_t* const runs = reinterpret_cast<pair_t*>(scratch) + 9 * lane;
+  auto write = [&](pair_t* p, int step) __attribute__((always_inline)) {
+    wave_lds_sync();  // this wave's earlier accesses come first
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = row[16 * i + 2 * ((c >> 1) ^ (i & 7)) + (c & 1)];
-  wave_lds_sync();
-#pragma unroll
-  for (int h = 1; h < 16 && 16 * h < G; h <<= 1)
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if ((i & h) == 0) {
-        const double x = v[i], y = v[i + h];
-        v[i] = x + y;
-        v[i + h] = x - y;
-      }
-  if constexpr (G >= 512) {
+    for (int i = 0; i < 8; ++i) p[step * i] = pair_t{v[2 * i], v[2 * i + 1]};
+    wave_lds_sync();
+  };
+  auto read = [&](const pair_t* p, int step) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      lane_swap<16>(v[i], v[i + 8]);
-      const double x = v[i], y = v[i + 8];
-      v[i] = x + y;
-      v[i + 8] = x - y;
+      const pair_t u = p[step * i];
+      v[2 * i] = u[0];
+      v[2 * i + 1] = u[1];
     }
+  };
+  auto high = [&]() __attribute__((always_inline)) {
+    if constexpr (G >= 256) mx_butterflies<2>(v);
+    if constexpr (G >= 512) mx_butterflies<4>(v);
+    if constexpr (G >= 1024) mx_butterflies<8>(v);
+  };
+  auto low = [&]() __attribute__((always_inline)) {
+    mx_butterflies<2>(v);
+    mx_butterflies<4>(v);
+    mx_butterflies<8>(v);
+  };
+  if constexpr (!BACK) {
+    mx_butterflies<1>(v);
+    high();
+    write(pairs, 72);
+    read(middle, 8);
+  } else {
+    mx_butterflies<1>(v);
+    low();
+    write(runs, 1);
+    read(middle, 9);
   }
-  if constexpr (G == 1024) {
-#pragma unroll
-    for (int h = 0; h < 16; h += 8)
-#pragma unroll
-      for (int i = h; i < h + 4; ++i) {
-        lane_swap<32>(v[i], v[i + 4]);
-        const double x = v[i], y = v[i + 4];
-        v[i] = x + y;
-        v[i + 4] = x - y;
-      }
+  mx_butterflies<2>(v);
+  mx_butterflies<4>(v);
+  if constexpr (G >= 128) mx_butterflies<8>(v);
+  if constexpr (!BACK) {
+    write(middle, 9);
+    read(runs, 1);
+    low();
+  } else {
+    write(middle, 8);
+    read(pairs, 72);
+    high();
   }
 }
 
@@ -184,113 +216,127 @@ __device__ inline float odd_scaled(double v, double inverse) {
 template <int G>
 constexpr int kRootShift = G == 64 ? 3 : G == 256 ? 4 : G == 1024 ? 5 : G == 4096 ? 6 : 0;
 
-// Largest of v over the 16 lanes of a DPP row, in all of them.
-__device__ inline uint32_t row_max(uint32_t v) {
-  v = max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x128, 0xF, 0xF, true)));  // row_ror:8
-  v = max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x124, 0xF, 0xF, true)));
-  v = max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x122, 0xF, 0xF, true)));
-  return max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x121, 0xF, 0xF, true)));
+// Signs of the lane's pairs: bit 15 of word r that of the first value, bit 31 that of
+// the second.
+struct MxPairSigns {
+  uint32_t m[8];
+};
+__device__ inline MxPairSigns pair_signs(const MxSigns& s, int lane) {
+  const uint32_t w = s.w[lane];
+  MxPairSigns p;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) p.m[r] = (w << (15 - r)) & 0x80008000u;
+  return p;
 }
 
-// Place of element n of a segment of 1024 in LDS: runs of 16 permuted so that
-// the four rows of lanes hit distinct banks.
-__device__ inline int lds_place(int n) { return n ^ ((((n >> 6) ^ (n >> 8)) & 3) << 4); }
-
-// Moves 16 fp32 values per lane from mx_fwht_rows's places to 16 consecutive ones
-// per lane through the wave's LDS.
-template <int G>
-__device__ inline void rows_to_lanes(float (&v)[16], float* lds, int lane) {
-  wave_lds_sync();
+// A lane's pairs as loaded.
+template <typename InT>
+struct MxPairs {
+  static constexpr int kWords = sizeof(InT) == 2 ? 1 : 2;  // per pair
+  uint32_t u[8 * kWords];
+};
+// Of the n values (a multiple of 64) from p on; zeros behind them.
+template <typename InT>
+__device__ inline MxPairs<InT> load_pairs(const InT* p, int64_t n, int lane) {
+  constexpr int kWords = MxPairs<InT>::kWords;
+  MxPairs<InT> w;
+  auto load = [&](int r) __attribute__((always_inline)) {
+    const uint32_t* const q = reinterpret_cast<const uint32_t*>(p + 128 * r + 2 * lane);
 #pragma unroll
-  for (int r = 0; r < 16; ++r) lds[lds_place(fwht_rows_lane<G>(lane) + fwht_rows_reg<G>(r))] = v[r];
-  wave_lds_sync();
-  typedef float f32x4 __attribute__((ext_vector_type(4)));
-  const f32x4* p = reinterpret_cast<const f32x4*>(lds + lds_place(16 * lane));
+    for (int i = 0; i < kWords; ++i) w.u[kWords * r + i] = q[i];
+  };
+  if (n >= 1024) {
 #pragma unroll
-  for (int h = 0; h < 4; ++h) {
-    const f32x4 u = p[h];
+    for (int r = 0; r < 8; ++r) load(r);
+  } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[4 * h + i] = u[i];
+    for (int r = 0; r < 8; ++r) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w.u[kWords * r + i] = 0;
+      if (128 * r + 2 * lane < n) load(r);
+    }
   }
-  wave_lds_sync();
+  return w;
 }
-// And back.
-template <int G>
-__device__ inline void lanes_to_rows(float (&v)[16], float* lds, int lane) {
-  wave_lds_sync();
-  typedef float f32x4 __attribute__((ext_vector_type(4)));
-  f32x4* p = reinterpret_cast<f32x4*>(lds + lds_place(16 * lane));
+// With their signs, in fp64.
+template <typename InT>
+__device__ inline void signed_pairs(const MxPairs<InT>& w, const MxPairSigns& s, double (&v)[16]) {
 #pragma unroll
-  for (int h = 0; h < 4; ++h) p[h] = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-  wave_lds_sync();
-#pragma unroll
-  for (int r = 0; r < 16; ++r) v[r] = lds[lds_place(fwht_rows_lane<G>(lane) + fwht_rows_reg<G>(r))];
-  wave_lds_sync();
+  for (int r = 0; r < 8; ++r) {
+    uint32_t a, b;
+    if constexpr (sizeof(InT) == 2) {
+      b = (w.u[r] ^ s.m[r]) & 0xffff0000u;
+      a = (w.u[r] ^ s.m[r]) << 16;
+    } else {
+      a = w.u[2 * r] ^ (s.m[r] << 16);
+      b = w.u[2 * r + 1] ^ (s.m[r] & 0x80000000u);
+    }
+    v[2 * r] = double(__builtin_bit_cast(float, a));
+    v[2 * r + 1] = double(__builtin_bit_cast(float, b));
+  }
 }
 
-// This lane's 16 sign bits for elements 16 lane .. of a segment of 1024.
-template <int G>
-__device__ inline uint32_t lane_signs(const MxSigns& s, int lane) {
-  const int j = (16 * lane) & (G - 1);
-  return s.w[j >> 5] >> (j & 16);
-}
-
-// x with the signs of the lane's 16 values (bit i of neg), in fp64.
-__device__ inline void signed_f64(const float (&x)[16], uint32_t neg, double (&v)[16]) {
+// The way back: n values from pairs, with their signs.
+template <typename OutT>
+__device__ inline void store_pairs(OutT* p, int64_t n, const MxPairSigns& s, int lane,
+                                   const float (&v)[16]) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  auto store = [&](int r) __attribute__((always_inline)) {
+    if constexpr (sizeof(OutT) == 2) {
+      *reinterpret_cast<uint32_t*>(p + 128 * r + 2 * lane) =
+          pack_bf16(v[2 * r], v[2 * r + 1]) ^ s.m[r];
+    } else {
+      const uint32_t a = __builtin_bit_cast(uint32_t, v[2 * r]) ^ (s.m[r] << 16);
+      const uint32_t b = __builtin_bit_cast(uint32_t, v[2 * r + 1]) ^ (s.m[r] & 0x80000000u);
+      *reinterpret_cast<f32x2*>(p + 128 * r + 2 * lane) =
+          f32x2{__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+    }
+  };
+  if (n >= 1024) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    v[i] = double(__builtin_bit_cast(
-        float, __builtin_bit_cast(uint32_t, x[i]) ^ ((neg << (31 - i)) & 0x80000000u)));
+    for (int r = 0; r < 8; ++r) store(r);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      if (128 * r + 2 * lane < n) store(r);
+  }
 }
 
-// Rotates a segment of 1024 values (groups of G), 16 consecutive ones per lane in
-// x, and quantizes it: codes of the lane's 16 values of the result (consecutive
-// ones again), and in lanes with lane % 16 < 8 the scale byte of block *block of
-// the segment. neg: the lane's sign bits; lds: the wave's kMxWaveLds dwords.
+// Rotates a segment of 1024 values (groups of G), in pairs in v, and quantizes it: codes
+// of values 16 lane .. 16 lane + 15 of the result, and the scale byte of their block, lane
+// / 2, in both its lanes. lds: the wave's kMxWaveLds<double> dwords.
 template <int G, int FMT>
-__device__ inline void mx_rotate_segment(float (&x)[16], uint32_t neg, double root, uint32_t* lds,
-                                         int lane, uint32_t (&c)[kWords16<FMT>], uint32_t* byte,
-                                         int* block) {
+__device__ inline void mx_rotate_segment(double (&v)[16], double root, uint32_t* lds, int lane,
+                                         uint32_t (&c)[kWords16<FMT>], uint32_t* byte) {
   constexpr int kShift = kRootShift<G>;
-  double v[16];
-  signed_f64(x, neg, v);
-  mx_fwht_rows<G>(v, lds, lane);
+  mx_fwht<G, false>(v, lds, lane);
   if constexpr (kShift == 0) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] *= root;
+    for (int i = 0; i < 16; ++i) v[i] *= root;
   }
-  // block b = r / 2: registers 2b and 2b + 1 of the row's 16 lanes. A NaN or an
-  // infinity of the input is in all values of its group: the larger of two is one too.
-  int of[8], top = 0;
+  // A NaN or an infinity of the input is in all values of its group: the larger of two
+  // is one too.
+  double m[8];
 #pragma unroll
-  for (int b = 0; b < 8; ++b) {
-    const double m = __builtin_fmax(__builtin_fabs(v[2 * b]), __builtin_fabs(v[2 * b + 1]));
-    const int f =
-        int(row_max(uint32_t(__builtin_bit_cast(uint64_t, m) >> 32) & 0x7fffffffu) >> 20) - kShift;
-    top = max(top, f);
-    of[b] = scale_exponent_f64(f);
+  for (int i = 0; i < 8; ++i)
+    m[i] = __builtin_fmax(__builtin_fabs(v[2 * i]), __builtin_fabs(v[2 * i + 1]));
+#pragma unroll
+  for (int n = 4; n > 0; n >>= 1)
+#pragma unroll
+    for (int i = 0; i < n; ++i) m[i] = __builtin_fmax(m[i], m[i + n]);
+  uint32_t hi = uint32_t(__builtin_bit_cast(uint64_t, m[0]) >> 32) & 0x7fffffffu;
+  hi = max(hi, uint32_t(lane_xor_small<1>(hi)));
+  const int field = int(hi >> 20) - kShift, e = scale_exponent_f64(field);
+  const double inverse = inverse_scale(e, kShift);
+  float x[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = odd_scaled(v[i], inverse);
+  *byte = uint32_t(e);
+  if (field >= kMxBad) {  // (kShift: an infinity's field is 2047)
+    *byte = 255;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
   }
-#pragma unroll
-  for (int r = 0; r < 16; ++r) x[r] = odd_scaled(v[r], inverse_scale(of[r / 2], kShift));
-  if (__any(top >= kMxBad)) {  // (kShift: an infinity's field is 2047)
-#pragma unroll
-    for (int b = 0; b < 8; ++b)
-      if (of[b] > 255 - kMxTop - 1) {
-        of[b] = 255;
-        x[2 * b] = x[2 * b + 1] = 0.f;
-      }
-  }
-  uint32_t mine = uint32_t(of[0]);
-  int e = fwht_rows_reg<G>(0);
-#pragma unroll
-  for (int b = 1; b < 8; ++b)
-    if ((lane & 7) == b) {
-      mine = uint32_t(of[b]);
-      e = fwht_rows_reg<G>(2 * b);
-    }
-  *byte = mine;
-  *block = (fwht_rows_lane<G>(lane & ~15) | e) / 32;
-  rows_to_lanes<G>(x, reinterpret_cast<float*>(lds), lane);
   mx_encode16<FMT>(x, c);
 }
 

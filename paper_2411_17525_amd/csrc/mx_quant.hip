@@ -10,9 +10,7 @@
 // codes are those of the exact rotation.
 //
 // With a rotation, a wavefront takes segments of 1024 values (of g for g =
-// 2048 and 4096): 16 consecutive values per lane, rotated by mx_fwht_rows, which
-// leaves a block in the 16 lanes of a DPP row and two registers. Rows are whole
-// groups there, so the matrix is one run of groups.
+// 2048 and 4096). Rows are whole groups there, so the matrix is one run of groups.
 
 #include <algorithm>
 #include <cmath>
@@ -40,8 +38,13 @@ void mx_signs(uint64_t seed, int g, MxSigns* s) {
   e.g = g;
   e.seed = seed;
   for (uint32_t& w : e.s.w) w = 0;
-  for (int j = 0; j < g; ++j)
-    if (rht_sign_negative(seed, uint32_t(j))) e.s.w[j / 32] |= 1u << (j % 32);
+  for (int j = 0; j < g; ++j) {
+    if (!rht_sign_negative(seed, uint32_t(j))) continue;
+    if (g > 1024)
+      e.s.w[j / 32] |= 1u << (j % 32);
+    else
+      for (int n = j; n < 1024; n += g) e.s.w[n / 2 % 64] |= 1u << (16 * (n % 2) + n / 128);
+  }
   *s = e.s;
 }
 
@@ -114,27 +117,24 @@ template <int G, int FMT, typename InT>
 __global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht(
     const InT* __restrict__ w, int64_t total, const MxSigns signs, double root,
     const RowSink sink) {
-  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds];
+  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds<double>];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  uint32_t* const lds = s_lds[wave];
-  const uint32_t neg = lane_signs<G>(signs, lane);
+  const MxPairSigns neg = pair_signs(signs, lane);
   const int64_t segs = (total + 1023) / 1024, step = int64_t(gridDim.x) * kWaves;
-  for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
-    const int64_t at = 1024 * seg + 16 * lane;
-    const bool live = at < total;  // total is a multiple of 64
-    float x[16];
-    if (live) {
-      load16(w + at, x);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 0.f;
-    }
+  int64_t seg = int64_t(blockIdx.x) * kWaves + wave;
+  MxPairs<InT> next = load_pairs(w + 1024 * seg, total - 1024 * seg, lane);
+  for (; seg < segs; seg += step) {
+    double v[16];
+    signed_pairs(next, neg, v);
+    const int64_t then = seg + step;
+    if (then < segs) next = load_pairs(w + 1024 * then, total - 1024 * then, lane);
     uint32_t c[kWords16<FMT>], byte;
-    int block;
-    mx_rotate_segment<G, FMT>(x, neg, root, lds, lane, c, &byte, &block);
-    if (live) sink.template put<FMT>(at / 16, c);
-    const int64_t mine = 32 * seg + block;
-    if ((lane & 15) < 8 && 32 * mine < total) sink.put_scale(mine, byte);
+    mx_rotate_segment<G, FMT>(v, root, s_lds[wave], lane, c, &byte);
+    const int64_t at = 1024 * seg + 16 * lane;
+    if (at < total) {  // total is a multiple of 64
+      sink.template put<FMT>(at / 16, c);
+      if ((lane & 1) == 0) sink.put_scale(at / 32, byte);
+    }
   }
 }
 
@@ -230,7 +230,8 @@ __global__ __launch_bounds__(64 * kTileRows) void mx_to_tiles(const InT* __restr
   __shared__ __attribute__((aligned(16))) uint8_t s_head[kUnits * 16];
   __shared__ __attribute__((aligned(16))) uint8_t s_tail[FMT == HIGGS_MX_FP6 ? kUnits * 8 : 16];
   __shared__ uint32_t s_scale[8 * kTileRows];
-  __shared__ __attribute__((aligned(16))) uint32_t s_lds[G > 0 ? kTileRows : 1][G > 0 ? kMxWaveLds : 4];
+  __shared__ __attribute__((aligned(16))) uint32_t
+      s_lds[G > 0 ? kTileRows : 1][G > 0 ? kMxWaveLds<double> : 4];
   if (int(blockIdx.x) >= blocks) {
     const int i = int(blockIdx.x) - blocks;
     scale_words(words, i / word_parts, i % word_parts, word_parts);
@@ -238,22 +239,19 @@ __global__ __launch_bounds__(64 * kTileRows) void mx_to_tiles(const InT* __restr
   }
   const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
   const int group = int(blockIdx.x) / segs, seg = int(blockIdx.x) - group * segs;
-  const int row = group * kTileRows + wave, k = 1024 * seg + 16 * lane;
+  const int row = group * kTileRows + wave;
   if (row < batch) {
-    const int left = in - k;
-    float v[16];
-    load16_upto(x + int64_t(row) * in + (left > 0 ? k : 0), left < 0 ? 0 : left > 16 ? 16 : left, v);
-    uint32_t c[kWords16<FMT>], byte;
-    int block;  // of the segment, whose scale byte this lane holds
-    bool holds;
+    const InT* const p = x + int64_t(row) * in;
+    uint32_t c[kWords16<FMT>], byte;  // (the scale byte of block lane / 2 of the segment)
     if constexpr (G > 0) {
-      mx_rotate_segment<G, FMT>(v, lane_signs<G>(signs, lane), root, s_lds[wave], lane, c, &byte,
-                                &block);
-      holds = (lane & 15) < 8;
+      double v[16];
+      signed_pairs(load_pairs(p + 1024 * seg, in - 1024 * seg, lane), pair_signs(signs, lane), v);
+      mx_rotate_segment<G, FMT>(v, root, s_lds[wave], lane, c, &byte);
     } else {
+      const int k = 1024 * seg + 16 * lane, left = in - k;
+      float v[16];
+      load16_upto(p + (left > 0 ? k : 0), left < 0 ? 0 : left > 16 ? 16 : left, v);
       byte = mx_plain_halves<FMT>(v, c);
-      block = lane >> 1;
-      holds = (lane & 1) == 0;
     }
     // half-block `lane` of the segment: block lane / 2, which is unit (lane / 2) * kTileRows + wave
     const int unit = (lane >> 1) * kTileRows + wave;
@@ -272,8 +270,8 @@ __global__ __launch_bounds__(64 * kTileRows) void mx_to_tiles(const InT* __restr
         tl[1] = c[2];
       }
     }
-    if (holds)
-      reinterpret_cast<uint8_t*>(s_scale)[((block >> 2) * kTileRows + wave) * 4 + (block & 3)] =
+    if ((lane & 1) == 0)
+      reinterpret_cast<uint8_t*>(s_scale)[((lane >> 3) * kTileRows + wave) * 4 + (lane >> 1 & 3)] =
           uint8_t(byte);
   }
   __syncthreads();
@@ -322,61 +320,29 @@ __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__
 
 // ---- the way back ----
 
-// Rotated back in fp32 (stored values are not decided at borders). Groups of 1024
-// through LDS (fwht1024_lds: 260 vector instructions per segment instead of 450, 39
-// instead of 52 us for 4096 x 14336 to bf16), which leaves four runs of four
-// consecutive values per lane; smaller groups in place, by DPP and permlane.
+// Rotated back in fp32 (stored values are not decided at borders): codes of 16
+// consecutive values per lane, values stored as pairs.
 template <int G, int FMT, typename OutT>
 __global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht(
     const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t total,
     const MxSigns signs, float root, OutT* __restrict__ w) {
-  constexpr bool kLds = G == 1024;
-  __shared__ __attribute__((aligned(16))) float s_lds[kLds ? kWaves : 1][kLds ? kFwht1024Scratch : 4];
+  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds<float>];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  // signs of the values that the lane ends with
-  uint32_t neg = 0;
-  if constexpr (kLds) {
-#pragma unroll
-    for (int h = 0; h < 4; ++h)
-      neg |= ((signs.w[8 * h + (lane >> 3)] >> (4 * lane & 31)) & 15) << (4 * h);
-  } else {
-    neg = lane_signs<G>(signs, lane);
-  }
+  const MxPairSigns neg = pair_signs(signs, lane);
   const int64_t segs = (total + 1023) / 1024, step = int64_t(gridDim.x) * kWaves;
   for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
     const int64_t at = 1024 * seg + 16 * lane;
-    const bool live = at < total;
     uint32_t c[kWords16<FMT>] = {}, byte = 0;
-    if (live) {
+    if (at < total) {
       load_codes16<FMT>(codes + (at / 16) * (4 * kWords16<FMT>), c);
       byte = scales[at / 32];
     }
-    float x[16], s = root;
+    float x[16];
     mx_decode16<FMT>(c, byte, x);
-    if constexpr (kLds) {
-      fwht1024_lds(x, s_lds[wave], lane);
-    } else {
-      fwht_in_lane<16>(x);
-      s *= fwht_cross_lane_deferred_fixed<16, G>(x, lane);
-    }
+    mx_fwht<G, true>(x, s_lds[wave], lane);
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      x[i] = __builtin_bit_cast(
-          float, __builtin_bit_cast(uint32_t, x[i] * s) ^ ((neg << (31 - i)) & 0x80000000u));
-    if constexpr (kLds) {
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        OutT* const p = w + 1024 * seg + 256 * h + 4 * lane;
-        if constexpr (sizeof(OutT) == 2)
-          *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x[4 * h], x[4 * h + 1]),
-                                                    pack_bf16(x[4 * h + 2], x[4 * h + 3]));
-        else
-          *reinterpret_cast<float4*>(p) =
-              make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
-      }
-    } else if (live) {
-      store16(w + at, x);
-    }
+    for (int i = 0; i < 16; ++i) x[i] *= root;
+    store_pairs(w + 1024 * seg, total - 1024 * seg, neg, lane, x);
   }
 }
 
@@ -457,38 +423,42 @@ __global__ __launch_bounds__(64 * kWaves) void mx_error_rht(
     const InT* __restrict__ w, int64_t in, const MxSigns signs, double root,
     const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
     double* __restrict__ row_err) {
-  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds];
+  __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds<double>];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  uint32_t* const lds = s_lds[wave];
-  const uint32_t neg = lane_signs<G>(signs, lane);
+  const MxPairSigns neg = pair_signs(signs, lane);
   const int64_t row = blockIdx.x;
   const InT* const wr = w + row * in;
   const uint8_t* const cr = codes + row * (in / 2);
   const uint8_t* const sr = scales + row * (in / 32);
   double err = 0.0, norm = 0.0;
-  for (int64_t k0 = 1024 * wave; k0 < in; k0 += 1024 * kWaves) {
+  // (the next segment's loads in flight)
+  struct {
+    MxPairs<InT> x;
+    uint32_t c[2], byte;
+  } next;
+  auto load = [&](int64_t k0) __attribute__((always_inline)) {
     const int64_t at = k0 + 16 * lane;
-    const bool live = at < in;
-    float x[16];
-    uint32_t c[2] = {0, 0}, byte = 0;
-    if (live) {
-      load16(wr + at, x);
-      load_codes16<HIGGS_MX_FP4>(cr + at / 2, c);
-      byte = sr[at / 32];
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    next.x = load_pairs(wr + k0, in - k0, lane);
+    next.c[0] = next.c[1] = next.byte = 0;
+    if (at < in) {
+      load_codes16<HIGGS_MX_FP4>(cr + at / 2, next.c);
+      next.byte = sr[at / 32];
     }
+  };
+  load(1024 * wave);
+  for (int64_t k0 = 1024 * wave; k0 < in; k0 += 1024 * kWaves) {
     double v[16];
-    signed_f64(x, neg, v);
+    signed_pairs(next.x, neg, v);
+    const uint32_t c[2] = {next.c[0], next.c[1]}, byte = next.byte;
+    if (k0 + 1024 * kWaves < in) load(k0 + 1024 * kWaves);
 #pragma unroll
     for (int i = 0; i < 16; ++i) norm = __builtin_fma(v[i], v[i], norm);
-    mx_decode16<HIGGS_MX_FP4>(c, byte, x);
-    mx_fwht_rows<G>(v, lds, lane);
-    lanes_to_rows<G>(x, reinterpret_cast<float*>(lds), lane);
+    mx_fwht<G, false>(v, s_lds[wave], lane);
+    float q[16];
+    mx_decode16<HIGGS_MX_FP4>(c, byte, q);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const double d = __builtin_fma(v[r], root, -double(x[r]));
+    for (int i = 0; i < 16; ++i) {
+      const double d = __builtin_fma(v[i], root, -double(q[i]));
       err = __builtin_fma(d, d, err);
     }
   }
