@@ -16,9 +16,9 @@ constexpr int kMxTop = 2;
 inline int mx_block_bytes(int fmt) { return fmt == HIGGS_MX_FP4 ? 16 : 24; }
 inline int64_t mx_blocks(int64_t in) { return (in + kMxBlock - 1) / kMxBlock; }
 
-// RHT signs, a bit set where sigma_j = -1: of a group of 2048 or 4096 bit j % 32 of word
-// j / 32; of smaller ones as the lanes hold a segment of 1024 values (bits r and 16 + r of
-// word l: values 128 r + 2 l and 128 r + 2 l + 1). A kernel argument.
+// RHT signs, a bit set where sigma_j = -1, as the lanes hold a group of 2048 or 4096, or
+// 1024 values of smaller ones: bits q % 16 and 16 + q % 16 of word 64 (q / 16) + l those of
+// values 128 q + 2 l and 128 q + 2 l + 1. A kernel argument.
 struct MxSigns {
   uint32_t w[128];
 };
@@ -109,15 +109,21 @@ __device__ inline void mx_encode16(const float (&v)[16], uint32_t* out) {
       out[h] = r;
     }
   } else {
-    // the instruction takes the even and the odd values of 32
+    // The instruction takes the even and the odd values of 32. It writes its first result
+    // before it has read all of them: as a builtin it got v[2:7] from v[0:15] and lost a
+    // value, so the result's registers are kept apart here.
     typedef float f32x16 __attribute__((ext_vector_type(16)));
+    typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
     f32x16 even = {}, odd = {};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       even[i] = v[2 * i];
       odd[i] = v[2 * i + 1];
     }
-    const auto r = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, 1.0f);
+    u32x6 r;
+    asm("v_cvt_scalef32_2xpk16_fp6_f32 %0, %1, %2, 1.0\n\ts_nop 1"
+        : "=&v"(r)
+        : "v"(even), "v"(odd));
 #pragma unroll
     for (int i = 0; i < 3; ++i) out[i] = r[i];
   }
@@ -142,8 +148,11 @@ __device__ inline void mx_decode16(const uint32_t* in, uint32_t byte, float (&v)
     }
   } else {
     typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
-    const auto r =
-        __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(u32x6{in[0], in[1], in[2], 0, 0, 0}, scale);
+    typedef float f32x32 __attribute__((ext_vector_type(32)));
+    f32x32 r;  // (registers of its own, as above)
+    asm("v_cvt_scalef32_pk32_f32_fp6 %0, %1, %2\n\ts_nop 1"
+        : "=&v"(r)
+        : "v"(u32x6{in[0], in[1], in[2], 0, 0, 0}), "v"(scale));
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = r[i];
   }

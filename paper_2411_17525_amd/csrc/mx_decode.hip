@@ -162,16 +162,16 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
     };
     if constexpr (G > 0) {
       uint32_t* const lds = reinterpret_cast<uint32_t*>(ring + (kRingSlots - 1) * kSlot);
-      const MxPairSigns neg = pair_signs(a.signs, lane);
+      MxLaneSigns<G> neg(a.signs, lane);
       const int segs = (a.in + 1023) / 1024;  // of a row; the last may end early
       for (int i = wave; i < batch * segs; i += waves) {
         const int b = i / segs, seg = i - b * segs;
         const int64_t at = int64_t(b) * a.in + 1024 * seg;
         double v[16];
         if (a.x_bf16)
-          signed_pairs(load_pairs(static_cast<const uint16_t*>(a.x) + at, a.in - 1024 * seg, lane), neg, v);
+          signed_pairs(load_pairs(static_cast<const uint16_t*>(a.x) + at, a.in - 1024 * seg, lane), neg.of(0), v);
         else
-          signed_pairs(load_pairs(static_cast<const float*>(a.x) + at, a.in - 1024 * seg, lane), neg, v);
+          signed_pairs(load_pairs(static_cast<const float*>(a.x) + at, a.in - 1024 * seg, lane), neg.of(0), v);
         uint32_t c[kWords16<FMT>], byte;
         mx_rotate_segment<G, FMT>(v, a.root, lds, lane, c, &byte);
         // (up to the end of the row's last stage: zeros behind its values)

@@ -197,9 +197,6 @@ __device__ inline uint32_t scale_byte_f32(uint32_t field) {
 // Exponent field of a double times 2^shift (11 bits plus shift), and the block's scale
 // byte from the largest: 2^128 or more, infinities and NaN are kMxBad or above.
 constexpr int kMxBad = 1023 + 128;
-__device__ inline int field_f64(double v) {
-  return int(uint32_t(__builtin_bit_cast(uint64_t, v) >> 52) & 0x7ff);
-}
 __device__ inline int scale_exponent_f64(int field) { return max(field - (1023 - 127 + kMxTop), 0); }
 // 2^-E / 2^shift for the scale exponent E + 127.
 __device__ inline double inverse_scale(int byte, int shift) {
@@ -216,18 +213,51 @@ __device__ inline float odd_scaled(double v, double inverse) {
 template <int G>
 constexpr int kRootShift = G == 64 ? 3 : G == 256 ? 4 : G == 1024 ? 5 : G == 4096 ? 6 : 0;
 
-// Signs of the lane's pairs: bit 15 of word r that of the first value, bit 31 that of
-// the second.
+// Groups of 2048 and 4096 are 2 and 4 segments, held by one wave: butterflies between
+// them, and of each as in a group of 1024.
+template <int G>
+constexpr int kSegments = G > 1024 ? G / 1024 : 1;
+template <int S, typename T>
+__device__ inline void mx_across(T (&v)[S][16]) {
+#pragma unroll
+  for (int h = 1; h < S; h <<= 1)
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      if ((s & h) == 0)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const T x = v[s][i], y = v[s + h][i];
+          v[s][i] = x + y;
+          v[s + h][i] = x - y;
+        }
+}
+
+// Signs of the lane's pairs of segment `seg` of a group: bit 15 of word r that of the
+// first value, bit 31 that of the second.
 struct MxPairSigns {
   uint32_t m[8];
 };
-__device__ inline MxPairSigns pair_signs(const MxSigns& s, int lane) {
-  const uint32_t w = s.w[lane];
-  MxPairSigns p;
+template <int G>
+struct MxLaneSigns {
+  uint32_t w[(kSegments<G> + 1) / 2];
+  __device__ MxLaneSigns(const MxSigns& s, int lane) {
 #pragma unroll
-  for (int r = 0; r < 8; ++r) p.m[r] = (w << (15 - r)) & 0x80008000u;
-  return p;
-}
+    for (int i = 0; i < (kSegments<G> + 1) / 2; ++i) w[i] = s.w[64 * i + lane];
+  }
+  __device__ MxPairSigns of(int seg) {
+    // (of several segments they are made anew each time, not kept over a loop: 16 and
+    // 32 registers)
+    if constexpr (kSegments<G> > 1) asm volatile("" : "+v"(w[seg >> 1]));
+    MxPairSigns p;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) p.m[r] = (w[seg >> 1] << (15 - r - 8 * (seg & 1))) & 0x80008000u;
+    return p;
+  }
+};
+// Waves per SIMD that a rotation's kernel is compiled for: its LDS and registers (32 per
+// segment for fp64 values) allow as many.
+template <int G>
+constexpr int kRotationWaves = kSegments<G> == 4 ? 2 : 4;
 
 // A lane's pairs as loaded.
 template <typename InT>
@@ -302,14 +332,15 @@ __device__ inline void store_pairs(OutT* p, int64_t n, const MxPairSigns& s, int
   }
 }
 
-// Rotates a segment of 1024 values (groups of G), in pairs in v, and quantizes it: codes
+// Rotates a segment of 1024 values (groups of G; of larger ones after mx_across), in
+// pairs in v, and quantizes it: codes
 // of values 16 lane .. 16 lane + 15 of the result, and the scale byte of their block, lane
 // / 2, in both its lanes. lds: the wave's kMxWaveLds<double> dwords.
 template <int G, int FMT>
 __device__ inline void mx_rotate_segment(double (&v)[16], double root, uint32_t* lds, int lane,
                                          uint32_t (&c)[kWords16<FMT>], uint32_t* byte) {
   constexpr int kShift = kRootShift<G>;
-  mx_fwht<G, false>(v, lds, lane);
+  mx_fwht<G < 1024 ? G : 1024, false>(v, lds, lane);
   if constexpr (kShift == 0) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] *= root;

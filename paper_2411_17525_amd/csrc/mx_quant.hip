@@ -40,10 +40,8 @@ void mx_signs(uint64_t seed, int g, MxSigns* s) {
   for (uint32_t& w : e.s.w) w = 0;
   for (int j = 0; j < g; ++j) {
     if (!rht_sign_negative(seed, uint32_t(j))) continue;
-    if (g > 1024)
-      e.s.w[j / 32] |= 1u << (j % 32);
-    else
-      for (int n = j; n < 1024; n += g) e.s.w[n / 2 % 64] |= 1u << (16 * (n % 2) + n / 128);
+    for (int n = j; n < std::max(g, 1024); n += g)
+      e.s.w[64 * (n / 2048) + n / 2 % 64] |= 1u << (16 * (n % 2) + n / 128 % 16);
   }
   *s = e.s;
 }
@@ -52,135 +50,34 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// Where a quantizer's kernel puts half-block u of the matrix (16 codes) and block
-// u's scale byte, u counted along the rows: the caller's arrays, row after row.
-struct RowSink {
-  uint8_t* codes;
-  uint8_t* scales;
-  template <int FMT>
-  __device__ void put(int64_t u, const uint32_t* c) const {
-    store_codes16<FMT>(codes + u * (4 * kWords16<FMT>), c);
-  }
-  __device__ void put_scale(int64_t u, uint32_t byte) const { scales[u] = uint8_t(byte); }
-};
-
-// The same into the product's layout (MxTiles). Rows of `halves` half-blocks (a
-// multiple of 4 with a rotation), u below 2^32.
-struct TileSink {
-  MxTiles t;
-  uint32_t halves;
-  template <int FMT>
-  __device__ void put_at(uint32_t row, uint32_t k, const uint32_t* c) const {
-    uint8_t* const unit = t.codes + mx_tile_unit<FMT>(t, row, k >> 1);
-    uint8_t* const head = unit + (row % 32 + (k >> 1) % 2 * 32) * 16;
-    if constexpr (FMT == HIGGS_MX_FP4) {
-      *reinterpret_cast<uint2*>(head + (k & 1) * 8) = make_uint2(c[0], c[1]);
-    } else {
-      // a block's 24 bytes are 16 and 8 apart: 12 of the first half, 4 + 8
-      uint32_t* const tail =
-          reinterpret_cast<uint32_t*>(unit + 1024 + (row % 32 + (k >> 1) % 2 * 32) * 8);
-      uint32_t* const h = reinterpret_cast<uint32_t*>(head);
-      if ((k & 1) == 0) {
-        h[0] = c[0];
-        h[1] = c[1];
-        h[2] = c[2];
-      } else {
-        h[3] = c[0];
-        tail[0] = c[1];
-        tail[1] = c[2];
-      }
-    }
-  }
-  __device__ void put_scale_at(uint32_t row, uint32_t kb, uint32_t byte) const {
-    t.scales[(int64_t(kb >> 2) * t.rows32 + row) * 4 + (kb & 3)] = uint8_t(byte);
-  }
-  template <int FMT>
-  __device__ void put(int64_t u, const uint32_t* c) const {
-    const uint32_t row = uint32_t(u) / halves, k = uint32_t(u) - row * halves;
-    put_at<FMT>(row, k, c);
-    // a row of 2 blocks more than whole stages: zeros up to the stage's end
-    if (k + 4 >= halves && ((halves >> 1) & 3) == 2) {
-      const uint32_t zero[3] = {0, 0, 0};
-      put_at<FMT>(row, k + 4, zero);
-    }
-  }
-  __device__ void put_scale(int64_t u, uint32_t byte) const {
-    const uint32_t blocks = halves >> 1, row = uint32_t(u) / blocks, kb = uint32_t(u) - row * blocks;
-    put_scale_at(row, kb, byte);
-    if (kb + 2 >= blocks && (blocks & 3) == 2) put_scale_at(row, kb + 2, 0);
-  }
-};
-
 // ---- quantization ----
 
 template <int G, int FMT, typename InT>
-__global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht(
+__global__ __launch_bounds__(64 * kWaves, kRotationWaves<G>) void mx_quantize_rht(
     const InT* __restrict__ w, int64_t total, const MxSigns signs, double root,
-    const RowSink sink) {
+    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+  constexpr int S = kSegments<G>;
   __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds<double>];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  const MxPairSigns neg = pair_signs(signs, lane);
-  const int64_t segs = (total + 1023) / 1024, step = int64_t(gridDim.x) * kWaves;
-  int64_t seg = int64_t(blockIdx.x) * kWaves + wave;
-  MxPairs<InT> next = load_pairs(w + 1024 * seg, total - 1024 * seg, lane);
-  for (; seg < segs; seg += step) {
-    double v[16];
-    signed_pairs(next, neg, v);
-    const int64_t then = seg + step;
-    if (then < segs) next = load_pairs(w + 1024 * then, total - 1024 * then, lane);
-    uint32_t c[kWords16<FMT>], byte;
-    mx_rotate_segment<G, FMT>(v, root, s_lds[wave], lane, c, &byte);
-    const int64_t at = 1024 * seg + 16 * lane;
-    if (at < total) {  // total is a multiple of 64
-      sink.template put<FMT>(at / 16, c);
-      if ((lane & 1) == 0) sink.put_scale(at / 32, byte);
-    }
-  }
-}
-
-// Groups of 2048 and 4096: E consecutive values per lane, one group per wave.
-template <int E, int FMT, typename InT, typename Sink>
-__global__ __launch_bounds__(64 * kWaves) void mx_quantize_rht_long(
-    const InT* __restrict__ w, int64_t total, const MxSigns signs, double root, const Sink sink) {
-  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  const int64_t segs = total / (64 * E), step = int64_t(gridDim.x) * kWaves;
-  for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
-    const int64_t at = 64 * E * seg + E * lane;
-    double v[E];
+  MxLaneSigns<G> neg(signs, lane);
+  const int64_t step = int64_t(gridDim.x) * kWaves * 1024 * S;
+  for (int64_t k = (int64_t(blockIdx.x) * kWaves + wave) * 1024 * S; k < total; k += step) {
+    double v[S][16];
 #pragma unroll
-    for (int q = 0; q < E / 16; ++q) {
-      float x[16];
-      load16(w + at + 16 * q, x);
-      const int j = E * lane + 16 * q;
-      const uint32_t neg = signs.w[j >> 5] >> (j & 16);
+    for (int s = 0; s < S; ++s)
+      signed_pairs(load_pairs(w + k + 1024 * s, S > 1 ? 1024 : total - k, lane),
+                   neg.of(s), v[s]);
+    mx_across(v);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[16 * q + i] = double((neg >> i) & 1 ? -x[i] : x[i]);
-    }
-    fwht_wave<E>(v, lane, 64 * E);
-    constexpr int kShift = kRootShift<64 * E>;
-    if constexpr (kShift == 0) {
-#pragma unroll
-      for (int i = 0; i < E; ++i) v[i] *= root;
-    }
-#pragma unroll
-    for (int b = 0; b < E / 32; ++b) {
-      int f = 0;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) f = max(f, field_f64(v[32 * b + i]));
-      f -= kShift;
-      const bool bad = f >= kMxBad;
-      const int byte = bad ? 255 : scale_exponent_f64(f);
-      const double inverse = inverse_scale(byte, kShift);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = bad ? 0.f : odd_scaled(v[32 * b + 16 * h + i], inverse);
-        uint32_t c[kWords16<FMT>];
-        mx_encode16<FMT>(x, c);
-        sink.template put<FMT>(at / 16 + 2 * b + h, c);
+    for (int s = 0; s < S; ++s) {
+      if (s > 0) __builtin_amdgcn_sched_barrier(0);  // (one segment's registers at a time)
+      uint32_t c[kWords16<FMT>], byte;
+      mx_rotate_segment<G, FMT>(v[s], root, s_lds[wave], lane, c, &byte);
+      const int64_t at = k + 1024 * s + 16 * lane;
+      if (S > 1 || at < total) {  // total is a multiple of 64 (and of groups)
+        store_codes16<FMT>(codes + (at / 16) * (4 * kWords16<FMT>), c);
+        if ((lane & 1) == 0) scales[at / 32] = uint8_t(byte);
       }
-      sink.put_scale(at / 32 + b, byte);
     }
   }
 }
@@ -220,7 +117,7 @@ constexpr int kTileRows = 4;
 
 template <int G, int FMT, typename InT>
 __global__ __launch_bounds__(64 * kTileRows) void mx_to_tiles(const InT* __restrict__ x, int batch,
-                                                              int in, int segs, int blocks,
+                                                              int in, int parts, int blocks,
                                                               const MxSigns signs, double root,
                                                               const MxTiles t,
                                                               const MxScaleWords words,
@@ -238,64 +135,77 @@ __global__ __launch_bounds__(64 * kTileRows) void mx_to_tiles(const InT* __restr
     return;
   }
   const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
-  const int group = int(blockIdx.x) / segs, seg = int(blockIdx.x) - group * segs;
-  const int row = group * kTileRows + wave;
-  if (row < batch) {
-    const InT* const p = x + int64_t(row) * in;
-    uint32_t c[kWords16<FMT>], byte;  // (the scale byte of block lane / 2 of the segment)
-    if constexpr (G > 0) {
-      double v[16];
-      signed_pairs(load_pairs(p + 1024 * seg, in - 1024 * seg, lane), pair_signs(signs, lane), v);
-      mx_rotate_segment<G, FMT>(v, root, s_lds[wave], lane, c, &byte);
-    } else {
-      const int k = 1024 * seg + 16 * lane, left = in - k;
-      float v[16];
-      load16_upto(p + (left > 0 ? k : 0), left < 0 ? 0 : left > 16 ? 16 : left, v);
-      byte = mx_plain_halves<FMT>(v, c);
-    }
-    // half-block `lane` of the segment: block lane / 2, which is unit (lane / 2) * kTileRows + wave
-    const int unit = (lane >> 1) * kTileRows + wave;
-    uint32_t* const h = reinterpret_cast<uint32_t*>(s_head + unit * 16);
-    if constexpr (FMT == HIGGS_MX_FP4) {
-      *reinterpret_cast<uint2*>(h + (lane & 1) * 2) = make_uint2(c[0], c[1]);
-    } else {
-      uint32_t* const tl = reinterpret_cast<uint32_t*>(s_tail + unit * 8);
-      if ((lane & 1) == 0) {
-        h[0] = c[0];
-        h[1] = c[1];
-        h[2] = c[2];
+  const int group = int(blockIdx.x) / parts, part = int(blockIdx.x) - group * parts;
+  const int row = group * kTileRows + wave, r0 = group * kTileRows;
+  const InT* const p = x + int64_t(row) * in;
+  constexpr int S = kSegments<G>;
+  double v[S][16];
+  if (G > 0 && row < batch) {
+    MxLaneSigns<G> neg(signs, lane);
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+      signed_pairs(load_pairs(p + 1024 * (S * part + s), S > 1 ? 1024 : in - 1024 * part, lane),
+                   neg.of(s), v[s]);
+    mx_across(v);
+  }
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    const int seg = S * part + s;
+    if (s > 0) __syncthreads();
+    if (row < batch) {
+      uint32_t c[kWords16<FMT>], byte;  // (the scale byte of block lane / 2 of the segment)
+      if constexpr (G > 0) {
+        mx_rotate_segment<G, FMT>(v[s], root, s_lds[wave], lane, c, &byte);
       } else {
-        h[3] = c[0];
-        tl[0] = c[1];
-        tl[1] = c[2];
+        const int k = 1024 * seg + 16 * lane, left = in - k;
+        float u[16];
+        load16_upto(p + (left > 0 ? k : 0), left < 0 ? 0 : left > 16 ? 16 : left, u);
+        byte = mx_plain_halves<FMT>(u, c);
       }
+      // half-block `lane` of the segment: block lane / 2, which is unit (lane / 2) * kTileRows +
+      // wave
+      const int unit = (lane >> 1) * kTileRows + wave;
+      uint32_t* const h = reinterpret_cast<uint32_t*>(s_head + unit * 16);
+      if constexpr (FMT == HIGGS_MX_FP4) {
+        *reinterpret_cast<uint2*>(h + (lane & 1) * 2) = make_uint2(c[0], c[1]);
+      } else {
+        uint32_t* const tl = reinterpret_cast<uint32_t*>(s_tail + unit * 8);
+        if ((lane & 1) == 0) {
+          h[0] = c[0];
+          h[1] = c[1];
+          h[2] = c[2];
+        } else {
+          h[3] = c[0];
+          tl[0] = c[1];
+          tl[1] = c[2];
+        }
+      }
+      if ((lane & 1) == 0)
+        reinterpret_cast<uint8_t*>(
+            s_scale)[((lane >> 3) * kTileRows + wave) * 4 + (lane >> 1 & 3)] = uint8_t(byte);
     }
-    if ((lane & 1) == 0)
-      reinterpret_cast<uint8_t*>(s_scale)[((lane >> 3) * kTileRows + wave) * 4 + (lane >> 1 & 3)] =
-          uint8_t(byte);
+    __syncthreads();
+    // unit u = (stage, half, block of the half, row); rows behind the batch are written
+    // too (of their own tile: never read as results)
+    const int stage0 = 8 * seg, stages = min(8, int(t.stages) - stage0);
+    uint8_t* const tile = t.codes + (int64_t(r0 / 32) * t.stages + stage0) * 2 * mx_half_bytes(FMT);
+    if (tid < kUnits) {
+      const int r = tid % kTileRows, blk = tid / kTileRows;  // blk = 4 stage + 2 half + j
+      if (blk < 4 * stages)
+        *reinterpret_cast<uint4*>(tile + (blk >> 1) * mx_half_bytes(FMT) +
+                                  ((blk & 1) * 32 + r0 % 32 + r) * 16) =
+            *reinterpret_cast<const uint4*>(s_head + tid * 16);
+    } else if (FMT == HIGGS_MX_FP6) {
+      const int u = tid - kUnits, r = u % kTileRows, blk = u / kTileRows;
+      if (blk < 4 * stages)
+        *reinterpret_cast<uint2*>(tile + (blk >> 1) * mx_half_bytes(FMT) + 1024 +
+                                  ((blk & 1) * 32 + r0 % 32 + r) * 8) =
+            *reinterpret_cast<const uint2*>(s_tail + u * 8);
+    }
+    if (tid < 8 * kTileRows && tid / kTileRows < stages)
+      *reinterpret_cast<uint32_t*>(t.scales + ((stage0 + tid / kTileRows) * t.rows32 + r0 +
+                                               tid % kTileRows) * 4) = s_scale[tid];
   }
-  __syncthreads();
-  // unit u = (stage, half, block of the half, row); rows behind the batch are written
-  // too (of their own tile: never read as results)
-  const int stage0 = 8 * seg, stages = min(8, int(t.stages) - stage0);
-  const int r0 = group * kTileRows;
-  uint8_t* const tile = t.codes + (int64_t(r0 / 32) * t.stages + stage0) * 2 * mx_half_bytes(FMT);
-  if (tid < kUnits) {
-    const int r = tid % kTileRows, blk = tid / kTileRows;  // blk = 4 stage + 2 half + j
-    if (blk < 4 * stages)
-      *reinterpret_cast<uint4*>(tile + (blk >> 1) * mx_half_bytes(FMT) +
-                                ((blk & 1) * 32 + r0 % 32 + r) * 16) =
-          *reinterpret_cast<const uint4*>(s_head + tid * 16);
-  } else if (FMT == HIGGS_MX_FP6) {
-    const int u = tid - kUnits, r = u % kTileRows, blk = u / kTileRows;
-    if (blk < 4 * stages)
-      *reinterpret_cast<uint2*>(tile + (blk >> 1) * mx_half_bytes(FMT) + 1024 +
-                                ((blk & 1) * 32 + r0 % 32 + r) * 8) =
-          *reinterpret_cast<const uint2*>(s_tail + u * 8);
-  }
-  if (tid < 8 * kTileRows && tid / kTileRows < stages)
-    *reinterpret_cast<uint32_t*>(
-        t.scales + ((stage0 + tid / kTileRows) * t.rows32 + r0 + tid % kTileRows) * 4) = s_scale[tid];
 }
 
 // No rotation: a lane takes 16 consecutive values, half a block. units: halves
@@ -303,7 +213,8 @@ __global__ __launch_bounds__(64 * kTileRows) void mx_to_tiles(const InT* __restr
 template <int FMT, typename InT>
 __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__ w, int64_t rows,
                                                          int64_t in, int64_t units,
-                                                         const RowSink sink) {
+                                                         uint8_t* __restrict__ codes,
+                                                         uint8_t* __restrict__ scales) {
   const int64_t total = rows * units, step = int64_t(gridDim.x) * 256;
   // (total is even, so both halves of a block are in range or neither is)
   for (int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x; u < total; u += step) {
@@ -313,8 +224,8 @@ __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__
     load16_upto(w + row * in + (left > 0 ? k : 0), int(left < 0 ? 0 : left > 16 ? 16 : left), x);
     uint32_t c[kWords16<FMT>];
     const uint32_t byte = mx_plain_halves<FMT>(x, c);
-    sink.template put<FMT>(u, c);
-    if ((u & 1) == 0) sink.put_scale(u / 2, byte);
+    store_codes16<FMT>(codes + u * (4 * kWords16<FMT>), c);
+    if ((u & 1) == 0) scales[u / 2] = uint8_t(byte);
   }
 }
 
@@ -323,59 +234,34 @@ __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__
 // Rotated back in fp32 (stored values are not decided at borders): codes of 16
 // consecutive values per lane, values stored as pairs.
 template <int G, int FMT, typename OutT>
-__global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht(
+__global__ __launch_bounds__(64 * kWaves, kRotationWaves<G>) void mx_dequantize_rht(
     const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t total,
     const MxSigns signs, float root, OutT* __restrict__ w) {
+  constexpr int S = kSegments<G>;
   __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds<float>];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  const MxPairSigns neg = pair_signs(signs, lane);
-  const int64_t segs = (total + 1023) / 1024, step = int64_t(gridDim.x) * kWaves;
-  for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
-    const int64_t at = 1024 * seg + 16 * lane;
-    uint32_t c[kWords16<FMT>] = {}, byte = 0;
-    if (at < total) {
-      load_codes16<FMT>(codes + (at / 16) * (4 * kWords16<FMT>), c);
-      byte = scales[at / 32];
+  MxLaneSigns<G> neg(signs, lane);
+  const int64_t step = int64_t(gridDim.x) * kWaves * 1024 * S;
+  for (int64_t k = (int64_t(blockIdx.x) * kWaves + wave) * 1024 * S; k < total; k += step) {
+    float x[S][16];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const int64_t at = k + 1024 * s + 16 * lane;
+      uint32_t c[kWords16<FMT>] = {}, byte = 0;
+      if (S > 1 || at < total) {
+        load_codes16<FMT>(codes + (at / 16) * (4 * kWords16<FMT>), c);
+        byte = scales[at / 32];
+      }
+      mx_decode16<FMT>(c, byte, x[s]);
     }
-    float x[16];
-    mx_decode16<FMT>(c, byte, x);
-    mx_fwht<G, true>(x, s_lds[wave], lane);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] *= root;
-    store_pairs(w + 1024 * seg, total - 1024 * seg, neg, lane, x);
-  }
-}
-
-template <int E, int FMT, typename OutT>
-__global__ __launch_bounds__(64 * kWaves) void mx_dequantize_rht_long(
-    const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t total,
-    const MxSigns signs, float root, OutT* __restrict__ w) {
-  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  const int64_t segs = total / (64 * E), step = int64_t(gridDim.x) * kWaves;
-  for (int64_t seg = int64_t(blockIdx.x) * kWaves + wave; seg < segs; seg += step) {
-    const int64_t at = 64 * E * seg + E * lane;
-    float v[E];
+    for (int s = 0; s < S; ++s) mx_fwht<G < 1024 ? G : 1024, true>(x[s], s_lds[wave], lane);
+    mx_across(x);
 #pragma unroll
-    for (int q = 0; q < E / 16; ++q) {
-      uint32_t c[kWords16<FMT>];
-      load_codes16<FMT>(codes + (at / 16 + q) * (4 * kWords16<FMT>), c);
-      float x[16];
-      mx_decode16<FMT>(c, scales[(at + 16 * q) / 32], x);
+    for (int s = 0; s < S; ++s) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[16 * q + i] = x[i];
-    }
-    fwht_in_lane<E>(v);
-    const float s = fwht_cross_lane_deferred_fixed<E, 64 * E>(v, lane) * root;
-#pragma unroll
-    for (int q = 0; q < E / 16; ++q) {
-      const int j = E * lane + 16 * q;
-      const uint32_t neg = signs.w[j >> 5] >> (j & 16);
-      float x[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        x[i] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v[16 * q + i] * s) ^
-                                             ((neg << (31 - i)) & 0x80000000u));
-      store16(w + at + 16 * q, x);
+      for (int i = 0; i < 16; ++i) x[s][i] *= root;
+      store_pairs(w + k + 1024 * s, S > 1 ? 1024 : total - k, neg.of(s), lane, x[s]);
     }
   }
 }
@@ -400,129 +286,95 @@ __global__ __launch_bounds__(256) void mx_dequantize_plain(const uint8_t* __rest
 
 // ---- layer error ----
 
-// A block per row: err = sum (v - q 2^E)^2 over the (rotated) row and norm =
-// sum w^2, fp64, summed in a fixed order.
-__device__ inline void row_sums(double err, double norm, int lane, int wave, double* row_err) {
-  __shared__ double s_sum[2][kWaves];
+// err = sum (v - q 2^E)^2 over a (rotated) row and norm = sum w^2, fp64, summed in a
+// fixed order. A block takes kWaves / split rows, a row `split` waves (1, 2 or 4).
+struct MxErrorRow {
+  int64_t row;
+  int part;  // this wave's of the row's
+  __device__ MxErrorRow(int split, int wave)
+      : row(int64_t(blockIdx.x) * (kWaves / split) + wave / split), part(wave % split) {}
+};
+__device__ inline void row_sums(double err, double norm, int lane, int wave, int split, int64_t rows,
+                                double* row_err) {
+  __shared__ double s_sum[kWaves][2];
   err = wave_sum(err, lane);
   norm = wave_sum(norm, lane);
   if (lane == 0) {
-    s_sum[0][wave] = err;
-    s_sum[1][wave] = norm;
+    s_sum[wave][0] = err;
+    s_sum[wave][1] = norm;
   }
   __syncthreads();
-  if (threadIdx.x < 2) {
+  const int here = kWaves / split, tid = int(threadIdx.x), r = tid >> 1;
+  const int64_t row = int64_t(blockIdx.x) * here + r;
+  if (r < here && row < rows) {
     double t = 0.0;
-    for (int q = 0; q < kWaves; ++q) t += s_sum[threadIdx.x][q];
-    row_err[2 * int64_t(blockIdx.x) + threadIdx.x] = t;
+    for (int q = 0; q < split; ++q) t += s_sum[r * split + q][tid & 1];
+    row_err[2 * row + (tid & 1)] = t;
   }
 }
 
 template <int G, typename InT>
-__global__ __launch_bounds__(64 * kWaves) void mx_error_rht(
-    const InT* __restrict__ w, int64_t in, const MxSigns signs, double root,
-    const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+__global__ __launch_bounds__(64 * kWaves, kSegments<G> == 2 ? 3 : kRotationWaves<G>) void mx_error_rht(
+    const InT* __restrict__ w, int64_t rows, int64_t in, int split, const MxSigns signs,
+    double root, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
     double* __restrict__ row_err) {
+  constexpr int S = kSegments<G>;
   __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds<double>];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  const MxPairSigns neg = pair_signs(signs, lane);
-  const int64_t row = blockIdx.x;
-  const InT* const wr = w + row * in;
-  const uint8_t* const cr = codes + row * (in / 2);
-  const uint8_t* const sr = scales + row * (in / 32);
+  const MxErrorRow mine(split, wave);
+  MxLaneSigns<G> neg(signs, lane);
   double err = 0.0, norm = 0.0;
-  // (the next segment's loads in flight)
-  struct {
-    MxPairs<InT> x;
-    uint32_t c[2], byte;
-  } next;
-  auto load = [&](int64_t k0) __attribute__((always_inline)) {
-    const int64_t at = k0 + 16 * lane;
-    next.x = load_pairs(wr + k0, in - k0, lane);
-    next.c[0] = next.c[1] = next.byte = 0;
-    if (at < in) {
-      load_codes16<HIGGS_MX_FP4>(cr + at / 2, next.c);
-      next.byte = sr[at / 32];
+  for (int64_t k = 1024 * S * mine.part; mine.row < rows && k < in; k += 1024 * S * split) {
+    const int64_t at = mine.row * in + k;
+    double v[S][16];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      if (s > 0) __builtin_amdgcn_sched_barrier(0);
+      signed_pairs(load_pairs(w + at + 1024 * s, S > 1 ? 1024 : in - k, lane),
+                   neg.of(s), v[s]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) norm = __builtin_fma(v[s][i], v[s][i], norm);
     }
-  };
-  load(1024 * wave);
-  for (int64_t k0 = 1024 * wave; k0 < in; k0 += 1024 * kWaves) {
-    double v[16];
-    signed_pairs(next.x, neg, v);
-    const uint32_t c[2] = {next.c[0], next.c[1]}, byte = next.byte;
-    if (k0 + 1024 * kWaves < in) load(k0 + 1024 * kWaves);
+    mx_across(v);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) norm = __builtin_fma(v[i], v[i], norm);
-    mx_fwht<G, false>(v, s_lds[wave], lane);
-    float q[16];
-    mx_decode16<HIGGS_MX_FP4>(c, byte, q);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const double d = __builtin_fma(v[i], root, -double(q[i]));
-      err = __builtin_fma(d, d, err);
-    }
-  }
-  row_sums(err, norm, lane, wave, row_err);
-}
-
-template <int E, typename InT>
-__global__ __launch_bounds__(64 * kWaves) void mx_error_rht_long(
-    const InT* __restrict__ w, int64_t in, const MxSigns signs, double root,
-    const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-    double* __restrict__ row_err) {
-  const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  const int64_t row = blockIdx.x;
-  double err = 0.0, norm = 0.0;
-  for (int64_t k0 = 64 * E * wave; k0 < in; k0 += 64 * E * kWaves) {
-    const int64_t at = row * in + k0 + E * lane;
-    double v[E];
-#pragma unroll
-    for (int q = 0; q < E / 16; ++q) {
-      float x[16];
-      load16(w + at + 16 * q, x);
-      const int j = E * lane + 16 * q;
-      const uint32_t neg = signs.w[j >> 5] >> (j & 16);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        v[16 * q + i] = double((neg >> i) & 1 ? -x[i] : x[i]);
-        norm = __builtin_fma(v[16 * q + i], v[16 * q + i], norm);
+    for (int s = 0; s < S; ++s) {
+      if (s > 0) __builtin_amdgcn_sched_barrier(0);
+      const int64_t here = at + 1024 * s + 16 * lane;
+      uint32_t c[2] = {0, 0}, byte = 0;
+      if (S > 1 || k + 16 * lane < in) {
+        load_codes16<HIGGS_MX_FP4>(codes + here / 2, c);
+        byte = scales[here / 32];
       }
-    }
-    fwht_wave<E>(v, lane, 64 * E);
-#pragma unroll
-    for (int q = 0; q < E / 16; ++q) {
-      uint32_t c[2];
-      load_codes16<HIGGS_MX_FP4>(codes + (at + 16 * q) / 2, c);
-      float x[16];
-      mx_decode16<HIGGS_MX_FP4>(c, scales[(at + 16 * q) / 32], x);
+      mx_fwht<G < 1024 ? G : 1024, false>(v[s], s_lds[wave], lane);
+      float q[16];
+      mx_decode16<HIGGS_MX_FP4>(c, byte, q);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const double d = __builtin_fma(v[16 * q + i], root, -double(x[i]));
+        const double d = __builtin_fma(v[s][i], root, -double(q[i]));
         err = __builtin_fma(d, d, err);
       }
     }
   }
-  row_sums(err, norm, lane, wave, row_err);
+  row_sums(err, norm, lane, wave, split, rows, row_err);
 }
 
 template <typename InT>
-__global__ __launch_bounds__(64 * kWaves) void mx_error_plain(const InT* __restrict__ w,
-                                                              int64_t in, int64_t units,
-                                                              const uint8_t* __restrict__ codes,
-                                                              const uint8_t* __restrict__ scales,
-                                                              double* __restrict__ row_err) {
+__global__ __launch_bounds__(64 * kWaves) void mx_error_plain(
+    const InT* __restrict__ w, int64_t rows, int64_t in, int64_t units, int split,
+    const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+    double* __restrict__ row_err) {
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-  const int64_t row = blockIdx.x;
+  const MxErrorRow mine(split, wave);
   double err = 0.0, norm = 0.0;
-  for (int64_t u = threadIdx.x; u < units; u += 64 * kWaves) {
+  for (int64_t u = 64 * mine.part + lane; mine.row < rows && u < units; u += 64 * split) {
     const int64_t left = in - 16 * u;
     if (left <= 0) continue;
     const int n = int(left > 16 ? 16 : left);
     float x[16], q[16];
-    load16_upto(w + row * in + 16 * u, n, x);
+    load16_upto(w + mine.row * in + 16 * u, n, x);
     uint32_t c[2];
-    load_codes16<HIGGS_MX_FP4>(codes + (row * units + u) * 8, c);
-    mx_decode16<HIGGS_MX_FP4>(c, scales[(row * units + u) / 2], q);
+    load_codes16<HIGGS_MX_FP4>(codes + (mine.row * units + u) * 8, c);
+    mx_decode16<HIGGS_MX_FP4>(c, scales[(mine.row * units + u) / 2], q);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (i < n) {
@@ -531,7 +383,7 @@ __global__ __launch_bounds__(64 * kWaves) void mx_error_plain(const InT* __restr
         err = __builtin_fma(d, d, err);
       }
   }
-  row_sums(err, norm, lane, wave, row_err);
+  row_sums(err, norm, lane, wave, split, rows, row_err);
 }
 
 __global__ __launch_bounds__(1024) void mx_t2(const double* __restrict__ row_err, int64_t rows,
@@ -560,10 +412,12 @@ __global__ __launch_bounds__(1024) void mx_t2(const double* __restrict__ row_err
   }
 }
 
-// Blocks for `waves` wavefronts of work, four to a block: at most eight blocks
-// per compute unit, the kernels loop over the rest.
-unsigned wave_blocks(int64_t waves) {
-  return unsigned(std::min<int64_t>((waves + kWaves - 1) / kWaves, 2048));
+// Blocks for segments (of G values) of `total`, a wave each, four to a block: at most
+// eight blocks per compute unit, the kernels loop over the rest.
+template <int G>
+unsigned segment_blocks(int64_t total) {
+  constexpr int64_t kBlock = 1024 * kSegments<G> * kWaves;
+  return unsigned(std::min<int64_t>((total + kBlock - 1) / kBlock, 2048));
 }
 unsigned unit_blocks(int64_t units) {
   return unsigned(std::min<int64_t>((units + 255) / 256, 1 << 20));
@@ -585,11 +439,11 @@ void for_group(int g, F f) {
 
 template <int FMT, typename InT>
 hipError_t quantize_typed(const InT* w, int64_t rows, int64_t in, int g, uint64_t seed,
-                          const RowSink& sink, hipStream_t stream) {
+                          uint8_t* codes, uint8_t* scales, hipStream_t stream) {
   if (g == 0) {
     const int64_t units = 2 * mx_blocks(in);
     hipLaunchKernelGGL((mx_quantize_plain<FMT, InT>), dim3(unit_blocks(rows * units)), dim3(256),
-                       0, stream, w, rows, in, units, sink);
+                       0, stream, w, rows, in, units, codes, scales);
     return hipGetLastError();
   }
   MxSigns signs;
@@ -598,15 +452,8 @@ hipError_t quantize_typed(const InT* w, int64_t rows, int64_t in, int g, uint64_
   const int64_t total = rows * in;
   for_group(g, [&](auto G) {
     constexpr int kG = decltype(G)::value;
-    if constexpr (kG <= 1024) {
-      hipLaunchKernelGGL((mx_quantize_rht<kG, FMT, InT>),
-                         dim3(wave_blocks((total + 1023) / 1024)), dim3(64 * kWaves), 0, stream, w,
-                         total, signs, root, sink);
-    } else {
-      hipLaunchKernelGGL((mx_quantize_rht_long<kG / 64, FMT, InT, RowSink>),
-                         dim3(wave_blocks(total / kG)), dim3(64 * kWaves), 0, stream, w, total,
-                         signs, root, sink);
-    }
+    hipLaunchKernelGGL((mx_quantize_rht<kG, FMT, InT>), dim3(segment_blocks<kG>(total)),
+                       dim3(64 * kWaves), 0, stream, w, total, signs, root, codes, scales);
   });
   return hipGetLastError();
 }
@@ -620,29 +467,16 @@ hipError_t tiles_typed(const InT* x, int64_t batch, int64_t in, int g, uint64_t 
     mx_signs(seed, g, &signs);
     root = 1.0 / std::sqrt(double(g));
   }
-  const int segs = int((in + 1023) / 1024);
-  int64_t blocks = (batch + kTileRows - 1) / kTileRows * segs;
-  if (g > 1024) {  // a wave per group, straight to memory
-    for_group(g, [&](auto G) {
-      constexpr int kG = decltype(G)::value;
-      if constexpr (kG > 1024)
-        hipLaunchKernelGGL((mx_quantize_rht_long<kG / 64, FMT, InT, TileSink>),
-                           dim3(wave_blocks(batch * in / kG)), dim3(64 * kWaves), 0, stream, x,
-                           batch * in, signs, root, TileSink{t, uint32_t(in / 16)});
-    });
-    blocks = 0;
-  }
-  const int parts = int(std::min<int64_t>((words.stages + 31) / 32, 64));
-  const int64_t word_blocks = words.to == nullptr ? 0 : (words.rows + 63) / 64 * parts;
-  if (blocks + word_blocks == 0) return hipGetLastError();
+  const int part = std::max(g, 1024), parts = int((in + part - 1) / part);
+  const int64_t blocks = (batch + kTileRows - 1) / kTileRows * parts;
+  const int word_parts = int(std::min<int64_t>((words.stages + 31) / 32, 64));
+  const int64_t word_blocks = words.to == nullptr ? 0 : (words.rows + 63) / 64 * word_parts;
   const auto launch = [&](auto G) {
-    constexpr int kG = decltype(G)::value;
-    if constexpr (kG <= 1024)
-      hipLaunchKernelGGL((mx_to_tiles<kG, FMT, InT>), dim3(unsigned(blocks + word_blocks)),
-                         dim3(64 * kTileRows), 0, stream, x, int(batch), int(in), segs,
-                         int(blocks), signs, root, t, words, parts);
+    hipLaunchKernelGGL((mx_to_tiles<decltype(G)::value, FMT, InT>),
+                       dim3(unsigned(blocks + word_blocks)), dim3(64 * kTileRows), 0, stream, x,
+                       int(batch), int(in), parts, int(blocks), signs, root, t, words, word_parts);
   };
-  if (g == 0 || g > 1024)
+  if (g == 0)
     launch(std::integral_constant<int, 0>{});
   else
     for_group(g, launch);
@@ -664,15 +498,8 @@ hipError_t dequantize_typed(const uint8_t* codes, const uint8_t* scales, int64_t
   const int64_t total = rows * in;
   for_group(g, [&](auto G) {
     constexpr int kG = decltype(G)::value;
-    if constexpr (kG <= 1024) {
-      hipLaunchKernelGGL((mx_dequantize_rht<kG, FMT, OutT>),
-                         dim3(wave_blocks((total + 1023) / 1024)), dim3(64 * kWaves), 0, stream,
-                         codes, scales, total, signs, root, w);
-    } else {
-      hipLaunchKernelGGL((mx_dequantize_rht_long<kG / 64, FMT, OutT>),
-                         dim3(wave_blocks(total / kG)), dim3(64 * kWaves), 0, stream, codes,
-                         scales, total, signs, root, w);
-    }
+    hipLaunchKernelGGL((mx_dequantize_rht<kG, FMT, OutT>), dim3(segment_blocks<kG>(total)),
+                       dim3(64 * kWaves), 0, stream, codes, scales, total, signs, root, w);
   });
   return hipGetLastError();
 }
@@ -681,24 +508,22 @@ template <typename InT>
 hipError_t error_typed(const InT* w, int64_t out, int64_t in, const uint8_t* codes,
                        const uint8_t* scales, int g, uint64_t seed, double* row_err,
                        hipStream_t stream) {
-  const dim3 grid{unsigned(out)}, block{64 * kWaves};
+  // waves of a row: one where the rows' waves fill the card, more of fewer rows
+  const int64_t segments = (in + std::max(g, 1024) - 1) / std::max(g, 1024);
+  int split = 1;
+  while (split < kWaves && out * split < 4096 && split < segments) split *= 2;
+  const dim3 grid{unsigned((out * split + kWaves - 1) / kWaves)}, block{64 * kWaves};
   if (g == 0) {
-    hipLaunchKernelGGL((mx_error_plain<InT>), grid, block, 0, stream, w, in, 2 * mx_blocks(in),
-                       codes, scales, row_err);
+    hipLaunchKernelGGL((mx_error_plain<InT>), grid, block, 0, stream, w, out, in,
+                       2 * mx_blocks(in), split, codes, scales, row_err);
     return hipGetLastError();
   }
   MxSigns signs;
   mx_signs(seed, g, &signs);
   const double root = 1.0 / std::sqrt(double(g));
   for_group(g, [&](auto G) {
-    constexpr int kG = decltype(G)::value;
-    if constexpr (kG <= 1024) {
-      hipLaunchKernelGGL((mx_error_rht<kG, InT>), grid, block, 0, stream, w, in, signs, root,
-                         codes, scales, row_err);
-    } else {
-      hipLaunchKernelGGL((mx_error_rht_long<kG / 64, InT>), grid, block, 0, stream, w, in, signs,
-                         root, codes, scales, row_err);
-    }
+    hipLaunchKernelGGL((mx_error_rht<decltype(G)::value, InT>), grid, block, 0, stream, w, out, in,
+                       split, signs, root, codes, scales, row_err);
   });
   return hipGetLastError();
 }
@@ -710,12 +535,11 @@ hipError_t launch_mx_quantize(const void* w, higgs_dtype dtype, int64_t rows, in
                               hipStream_t stream) {
   const float* wf = static_cast<const float*>(w);
   const uint16_t* wb = static_cast<const uint16_t*>(w);
-  const RowSink sink{codes, scales};
   if (fmt == HIGGS_MX_FP4)
-    return dtype == HIGGS_F32 ? quantize_typed<HIGGS_MX_FP4>(wf, rows, in, g, seed, sink, stream)
-                              : quantize_typed<HIGGS_MX_FP4>(wb, rows, in, g, seed, sink, stream);
-  return dtype == HIGGS_F32 ? quantize_typed<HIGGS_MX_FP6>(wf, rows, in, g, seed, sink, stream)
-                            : quantize_typed<HIGGS_MX_FP6>(wb, rows, in, g, seed, sink, stream);
+    return dtype == HIGGS_F32 ? quantize_typed<HIGGS_MX_FP4>(wf, rows, in, g, seed, codes, scales, stream)
+                              : quantize_typed<HIGGS_MX_FP4>(wb, rows, in, g, seed, codes, scales, stream);
+  return dtype == HIGGS_F32 ? quantize_typed<HIGGS_MX_FP6>(wf, rows, in, g, seed, codes, scales, stream)
+                            : quantize_typed<HIGGS_MX_FP6>(wb, rows, in, g, seed, codes, scales, stream);
 }
 
 hipError_t launch_mx_tiles(const void* x, higgs_dtype dtype, int64_t batch, int64_t in, int fmt,
