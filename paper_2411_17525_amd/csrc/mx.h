@@ -44,11 +44,6 @@ struct MxScaleWords {
   int blocks, stages;
 };
 constexpr int mx_half_bytes(int fmt) { return fmt == HIGGS_MX_FP4 ? 1024 : 1536; }
-// Offset of the half (1 or 1.5 KiB) that holds block kb of a row.
-template <int FMT>
-__host__ __device__ inline int64_t mx_tile_unit(const MxTiles& t, uint32_t row, uint32_t kb) {
-  return ((int64_t(row / 32) * t.stages + kb / 4) * 2 + kb / 2 % 2) * mx_half_bytes(FMT);
-}
 
 // Kernel launchers. g = 0: no rotation. The arguments have been checked.
 hipError_t launch_mx_quantize(const void* w, higgs_dtype dtype, int64_t rows, int64_t in, int fmt,

@@ -2,7 +2,7 @@
 //
 // A block takes tiles of 16 outputs, one after another; its waves share K in
 // chunks of 512 (256 bytes of a weight row). A wave's chunk of a tile, 4 KiB, goes
-// from memory into the wave's own LDS slots, RING chunks ahead and with whole lines
+// from memory into the wave's own LDS slots, one chunk ahead and with whole lines
 // of each row, and from there into the 16x16x128 scaled matrix instruction, whose
 // other operand is up to 16 activation rows; 32 with two of them. The waves' sums
 // of a tile meet in LDS and are added in the waves' order.
@@ -10,6 +10,12 @@
 // The activations come from the product's workspace (MxTiles), or, for calls that
 // convert little (FUSED), each block rotates and quantizes them itself while its
 // first weights are on their way, into LDS: one launch instead of two.
+//
+// What bounds it is the way from memory to LDS, and with few chunks per wave the
+// latency of a chunk (2.4 us): 4 x 4096 -> 28672 takes 13.7 us (62 MB, 4.5 TB/s), 16 x
+// 14336 -> 4096 15 us behind the conversion (31 MB, 2.1 TB/s), one row of 4096 -> 4096
+// 7.3 us, of which a launch and the conversion are half. 3 slots and 14 waves gained
+// nothing, two blocks per compute unit with two tiles of rows lost.
 
 #include <algorithm>
 
@@ -84,8 +90,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int row = 4 * j + q, unit = r16 ^ row;
-      const uint32_t at = uint32_t(min(int64_t(tile) * 16 + row, a.out - 1)) * uint32_t(a.blocks * 16) +
-                          uint32_t(chunk * 256 + unit * 16);
+      const int64_t o = min(int64_t(tile) * 16 + row, a.out - 1);
+      const uint32_t at = uint32_t(o) * uint32_t(a.blocks * 16) + uint32_t(chunk * 256 + unit * 16);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(wrs, (lds_void*)(ring + slot * kSlot + j * 1024), 16,
                                                int(at), 0, 0, 0);
     }
@@ -145,7 +151,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
         *reinterpret_cast<u32x2*>(head + (half & 1) * 8) = u32x2{c[0], c[1]};
       } else {
         uint32_t* const h = reinterpret_cast<uint32_t*>(head);
-        uint32_t* const t = reinterpret_cast<uint32_t*>(s_mem + kXTail + ((half >> 1) * batch + b) * 8);
+        uint32_t* const t =
+            reinterpret_cast<uint32_t*>(s_mem + kXTail + ((half >> 1) * batch + b) * 8);
         if ((half & 1) == 0) {
           h[0] = c[0];
           h[1] = c[1];
@@ -167,11 +174,12 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
       for (int i = wave; i < batch * segs; i += waves) {
         const int b = i / segs, seg = i - b * segs;
         const int64_t at = int64_t(b) * a.in + 1024 * seg;
+        const int left = a.in - 1024 * seg;
         double v[16];
         if (a.x_bf16)
-          signed_pairs(load_pairs(static_cast<const uint16_t*>(a.x) + at, a.in - 1024 * seg, lane), neg.of(0), v);
+          signed_pairs(load_pairs(static_cast<const uint16_t*>(a.x) + at, left, lane), neg.of(0), v);
         else
-          signed_pairs(load_pairs(static_cast<const float*>(a.x) + at, a.in - 1024 * seg, lane), neg.of(0), v);
+          signed_pairs(load_pairs(static_cast<const float*>(a.x) + at, left, lane), neg.of(0), v);
         uint32_t c[kWords16<FMT>], byte;
         mx_rotate_segment<G, FMT>(v, a.root, lds, lane, c, &byte);
         // (up to the end of the row's last stage: zeros behind its values)

@@ -197,7 +197,9 @@ __device__ inline uint32_t scale_byte_f32(uint32_t field) {
 // Exponent field of a double times 2^shift (11 bits plus shift), and the block's scale
 // byte from the largest: 2^128 or more, infinities and NaN are kMxBad or above.
 constexpr int kMxBad = 1023 + 128;
-__device__ inline int scale_exponent_f64(int field) { return max(field - (1023 - 127 + kMxTop), 0); }
+__device__ inline int scale_exponent_f64(int field) {
+  return max(field - (1023 - 127 + kMxTop), 0);
+}
 // 2^-E / 2^shift for the scale exponent E + 127.
 __device__ inline double inverse_scale(int byte, int shift) {
   return __builtin_bit_cast(double, uint64_t(uint32_t(1023 + 127 - shift - byte) << 20) << 32);

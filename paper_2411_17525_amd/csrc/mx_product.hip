@@ -2,7 +2,8 @@
 // (where g > 0) and converted to E2M1 or E2M3 blocks by the quantizer's kernel,
 // then multiplied by the scaled matrix instruction, which takes both operands'
 // codes and one power of two per 32 values of K and lane. Products of these
-// formats and their sums of 64 are exact in it; sums are fp32.
+// formats are exact in it (with E4M3 activations it drops low bits and runs at half
+// the rate, so those of more than 4 bits are E2M3); sums are fp32.
 //
 // Operands of v_mfma_scale_f32_32x32x64_f8f6f4 (either format): lane l holds
 // the block l / 32 of two (32 consecutive values of K) of row l % 32 and its
@@ -64,9 +65,9 @@ __device__ MX_INLINE inline void for_each(const F& f) {
 // A block computes tiles of BM activation rows x BN outputs over a range of K with
 // WM x WN waves, one after another, stage by stage of 128 values: the stage's
 // activations, weights and scale words go from memory to LDS, from there into the
-// operands. The loads run NB - 1/2 stages ahead. Weights are loaded for two stages at a time, 128 bytes of a
-// row: the address unit takes about as long for half a line as for a whole one
-// (62, 88 and 106 GB/s per compute unit in pieces of 64, 128 and 256 bytes), and
+// operands. The loads run NB - 1/2 stages ahead. Weights are loaded for two stages at
+// a time, 128 bytes of a row: the address unit takes about as long for half a line as
+// for a whole one (62, 88 and 106 GB/s per compute unit in pieces of 64, 128 and 256 bytes), and
 // that time is what the products have to hide. So that every stage loads as much,
 // the block's first half of columns has its pairs of stages at (0, 1), (2, 3) ..,
 // the second at (-1, 0), (1, 2) .. (NB is odd; a range of K has an even number of
@@ -398,7 +399,8 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
 
     // ---- outputs: register i holds row i % 4 + 8 (i / 4) + 4 hi, column r32 ----
     const bool partial = a.splits > 1;
-    const int64_t bw = int64_t(now.mt) * BM + wm * TM * 32, ow = int64_t(now.nt) * BN + wn * TN * 32;
+    const int64_t bw = int64_t(now.mt) * BM + wm * TM * 32;
+    const int64_t ow = int64_t(now.nt) * BN + wn * TN * 32;
     const int brows = int(min(a.batch - bw, int64_t(BM))) - 4 * hi;
     const int ocols = int(min(a.out - ow, int64_t(BN))) - r32;
     const bool full = a.batch - bw >= TM * 32 && a.out - ow >= TN * 32;
@@ -661,8 +663,8 @@ hipError_t launch_mx_qmatmul(const void* x, higgs_dtype x_dtype, int64_t batch, 
     st = launch_mx_tiles(x, x_dtype, batch, in, fmt, g, seed, a.x, w_scales, stream);
   if (st != hipSuccess) return st;
   if (p.main.shape < 0)
-    return launch_mx_decode(x, x_dtype, batch, fmt, a.x, codes, scales, g, seed, out, in, y, y_dtype,
-                            stream);
+    return launch_mx_decode(x, x_dtype, batch, fmt, a.x, codes, scales, g, seed, out, in, y,
+                            y_dtype, stream);
   a.wc = codes;
   a.ws = words;
   a.y = y;

@@ -11,6 +11,11 @@
 //
 // With a rotation, a wavefront takes segments of 1024 values (of g for g =
 // 2048 and 4096). Rows are whole groups there, so the matrix is one run of groups.
+// What bounds these kernels is the issue of vector instructions: of the 337 that a
+// segment's quantization takes (160 of them the butterflies, in fp64 at the rate of
+// fp32), 71% of the cycles issue one; LDS is busy in 41%. 14336 x 4096 bf16 to E2M1 with
+// g = 1024: 45 to 49 us (3.2 TB/s); its layer error 46 (3.2 TB/s), the way back 35 (4.2
+// TB/s, near a copy's rate).
 
 #include <algorithm>
 #include <cmath>
@@ -61,12 +66,19 @@ __global__ __launch_bounds__(64 * kWaves, kRotationWaves<G>) void mx_quantize_rh
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
   MxLaneSigns<G> neg(signs, lane);
   const int64_t step = int64_t(gridDim.x) * kWaves * 1024 * S;
-  for (int64_t k = (int64_t(blockIdx.x) * kWaves + wave) * 1024 * S; k < total; k += step) {
+  int64_t k = (int64_t(blockIdx.x) * kWaves + wave) * 1024 * S;
+  MxPairs<InT> next;  // one segment's values are loaded ahead (45 us for 14336 x 4096, not 50)
+  if constexpr (S == 1) next = load_pairs(w + k, total - k, lane);
+  for (; k < total; k += step) {
     double v[S][16];
+    if constexpr (S == 1) {
+      signed_pairs(next, neg.of(0), v[0]);
+      if (k + step < total) next = load_pairs(w + k + step, total - k - step, lane);
+    } else {
 #pragma unroll
-    for (int s = 0; s < S; ++s)
-      signed_pairs(load_pairs(w + k + 1024 * s, S > 1 ? 1024 : total - k, lane),
-                   neg.of(s), v[s]);
+      for (int s = 0; s < S; ++s)
+        signed_pairs(load_pairs(w + k + 1024 * s, 1024, lane), neg.of(s), v[s]);
+    }
     mx_across(v);
 #pragma unroll
     for (int s = 0; s < S; ++s) {
@@ -294,8 +306,8 @@ struct MxErrorRow {
   __device__ MxErrorRow(int split, int wave)
       : row(int64_t(blockIdx.x) * (kWaves / split) + wave / split), part(wave % split) {}
 };
-__device__ inline void row_sums(double err, double norm, int lane, int wave, int split, int64_t rows,
-                                double* row_err) {
+__device__ inline void row_sums(double err, double norm, int lane, int wave, int split,
+                                int64_t rows, double* row_err) {
   __shared__ double s_sum[kWaves][2];
   err = wave_sum(err, lane);
   norm = wave_sum(norm, lane);
@@ -314,7 +326,8 @@ __device__ inline void row_sums(double err, double norm, int lane, int wave, int
 }
 
 template <int G, typename InT>
-__global__ __launch_bounds__(64 * kWaves, kSegments<G> == 2 ? 3 : kRotationWaves<G>) void mx_error_rht(
+__global__ __launch_bounds__(64 * kWaves, kSegments<G> == 2 ? 3 : kRotationWaves<G>)
+void mx_error_rht(
     const InT* __restrict__ w, int64_t rows, int64_t in, int split, const MxSigns signs,
     double root, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
     double* __restrict__ row_err) {
@@ -324,30 +337,47 @@ __global__ __launch_bounds__(64 * kWaves, kSegments<G> == 2 ? 3 : kRotationWaves
   const MxErrorRow mine(split, wave);
   MxLaneSigns<G> neg(signs, lane);
   double err = 0.0, norm = 0.0;
-  for (int64_t k = 1024 * S * mine.part; mine.row < rows && k < in; k += 1024 * S * split) {
-    const int64_t at = mine.row * in + k;
+  int64_t k = 1024 * S * mine.part;
+  const int64_t step = 1024 * S * split, end = mine.row < rows ? in : 0, row0 = mine.row * in;
+  // one bf16 segment's loads go ahead (45 us for 4096 x 14336, not 48; fp32 ones spill)
+  constexpr bool kAhead = S == 1 && sizeof(InT) == 2;
+  struct {
+    MxPairs<InT> x;
+    uint32_t c[2], byte;
+  } next;
+  auto load = [&](int64_t at) __attribute__((always_inline)) {
+    next.x = load_pairs(w + row0 + at, S > 1 ? 1024 : end - at, lane);
+    next.c[0] = next.c[1] = next.byte = 0;
+    const int64_t here = row0 + at + 16 * lane;
+    if (S > 1 || at + 16 * lane < end) {
+      load_codes16<HIGGS_MX_FP4>(codes + here / 2, next.c);
+      next.byte = scales[here / 32];
+    }
+  };
+  if constexpr (kAhead) load(k);
+  for (; k < end; k += step) {
     double v[S][16];
+    uint32_t c[S][2], byte[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      if (s > 0) __builtin_amdgcn_sched_barrier(0);
-      signed_pairs(load_pairs(w + at + 1024 * s, S > 1 ? 1024 : in - k, lane),
-                   neg.of(s), v[s]);
+      __builtin_amdgcn_sched_barrier(0);  // (one segment's registers at a time)
+      if constexpr (!kAhead) load(k + 1024 * s);
+      signed_pairs(next.x, neg.of(s), v[s]);
+      c[s][0] = next.c[0];
+      c[s][1] = next.c[1];
+      byte[s] = next.byte;
+      if constexpr (kAhead)
+        if (k + step < end) load(k + step);
 #pragma unroll
       for (int i = 0; i < 16; ++i) norm = __builtin_fma(v[s][i], v[s][i], norm);
     }
     mx_across(v);
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      if (s > 0) __builtin_amdgcn_sched_barrier(0);
-      const int64_t here = at + 1024 * s + 16 * lane;
-      uint32_t c[2] = {0, 0}, byte = 0;
-      if (S > 1 || k + 16 * lane < in) {
-        load_codes16<HIGGS_MX_FP4>(codes + here / 2, c);
-        byte = scales[here / 32];
-      }
+      __builtin_amdgcn_sched_barrier(0);
       mx_fwht<G < 1024 ? G : 1024, false>(v[s], s_lds[wave], lane);
       float q[16];
-      mx_decode16<HIGGS_MX_FP4>(c, byte, q);
+      mx_decode16<HIGGS_MX_FP4>(c[s], byte[s], q);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const double d = __builtin_fma(v[s][i], root, -double(q[i]));
@@ -508,7 +538,8 @@ template <typename InT>
 hipError_t error_typed(const InT* w, int64_t out, int64_t in, const uint8_t* codes,
                        const uint8_t* scales, int g, uint64_t seed, double* row_err,
                        hipStream_t stream) {
-  // waves of a row: one where the rows' waves fill the card, more of fewer rows
+  // waves of a row: one where the rows' waves fill the card, more of fewer rows (14336 x
+  // 4096, g = 1024: 46 us with one, 58 with four; 1000 x 4096: 8.2 and 7.4)
   const int64_t segments = (in + std::max(g, 1024) - 1) / std::max(g, 1024);
   int split = 1;
   while (split < kWaves && out * split < 4096 && split < segments) split *= 2;
@@ -533,13 +564,13 @@ hipError_t error_typed(const InT* w, int64_t out, int64_t in, const uint8_t* cod
 hipError_t launch_mx_quantize(const void* w, higgs_dtype dtype, int64_t rows, int64_t in, int fmt,
                               int g, uint64_t seed, uint8_t* codes, uint8_t* scales,
                               hipStream_t stream) {
-  const float* wf = static_cast<const float*>(w);
-  const uint16_t* wb = static_cast<const uint16_t*>(w);
-  if (fmt == HIGGS_MX_FP4)
-    return dtype == HIGGS_F32 ? quantize_typed<HIGGS_MX_FP4>(wf, rows, in, g, seed, codes, scales, stream)
-                              : quantize_typed<HIGGS_MX_FP4>(wb, rows, in, g, seed, codes, scales, stream);
-  return dtype == HIGGS_F32 ? quantize_typed<HIGGS_MX_FP6>(wf, rows, in, g, seed, codes, scales, stream)
-                            : quantize_typed<HIGGS_MX_FP6>(wb, rows, in, g, seed, codes, scales, stream);
+  const auto run = [&](const auto* p) {
+    return fmt == HIGGS_MX_FP4
+               ? quantize_typed<HIGGS_MX_FP4>(p, rows, in, g, seed, codes, scales, stream)
+               : quantize_typed<HIGGS_MX_FP6>(p, rows, in, g, seed, codes, scales, stream);
+  };
+  return dtype == HIGGS_F32 ? run(static_cast<const float*>(w))
+                            : run(static_cast<const uint16_t*>(w));
 }
 
 hipError_t launch_mx_tiles(const void* x, higgs_dtype dtype, int64_t batch, int64_t in, int fmt,
