@@ -189,7 +189,10 @@ def _mx_workspace(batch, out, inp, fmt, g):
 
 
 def _of_sizes(kept, *sizes):
-    return (kept if all(type(v) is int for v in sizes) else kept.__wrapped__)(*sizes)
+    for v in sizes:
+        if type(v) is not int:
+            return kept.__wrapped__(*sizes)
+    return kept(*sizes)
 
 
 def _new_f32(like, rows, cols):
@@ -564,11 +567,17 @@ def _need_matrix(name, t, dtypes):
         raise ValueError(f"{name} must have two dimensions")
 
 
-def _need_beside(like, **tensors):
-    """Every tensor given on like's device."""
-    for name, t in tensors.items():
-        if t is not None and t.device != like.device:
-            raise ValueError(f"{name} must be on {like.device}, like the input")
+def _mx_stream(stream, first, *tensors):
+    """The call's stream (the current one), which is to be on the device of all tensors."""
+    device = first.get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
+    cuda = _torch._C
+    on = cuda._cuda_getDevice() if stream is None else stream.device.index
+    if on != device:
+        raise ValueError(f"tensors on {first.device}, stream on cuda:{on}")
+    return cuda._cuda_getCurrentRawStream(on) if stream is None else int(stream.cuda_stream)
 
 
 def _need_mx_layer(codes, scales, rows, inp, fmt):
@@ -610,9 +619,9 @@ def mx_quantize(w, fmt: int = MX_FP4, g: int = 0, seed: int = 0, codes=None, sca
     codes = _new(w, rows, cb, _torch.uint8) if codes is None else codes
     scales = _new(w, rows, sb, _torch.uint8) if scales is None else scales
     _need_mx_layer(codes, scales, rows, inp, fmt)
-    _need_beside(w, codes=codes, scales=scales)
+    on = _mx_stream(stream, w, codes, scales)
     _check(lib().higgs_mx_quantize(_ptr(w), _dtype_code(w), rows, inp, fmt, g, seed, _ptr(codes),
-                                   _ptr(scales), _stream(stream)))
+                                   _ptr(scales), on))
     return codes, scales
 
 
@@ -630,9 +639,9 @@ def mx_dequantize(codes, scales, in_features: int, fmt: int = MX_FP4, g: int = 0
     _need_cuda("out", out, (dtype,))
     if out.numel() < rows * in_features:
         raise ValueError("out buffer too small")
-    _need_beside(codes, scales=scales, out=out)
+    on = _mx_stream(stream, codes, scales, out)
     _check(lib().higgs_mx_dequantize(_ptr(codes), _ptr(scales), rows, in_features, fmt, g, seed,
-                                     _ptr(out), _dtype_code(out), _stream(stream)))
+                                     _ptr(out), _dtype_code(out), on))
     return out
 
 
@@ -652,9 +661,9 @@ def mx_layer_error(w, codes, scales, g: int = 0, seed: int = 0, row_err=None, t2
     _need_cuda("t2", t2, f64)
     if row_err.numel() < 2 * out or t2.numel() < 1:
         raise ValueError("row_err or t2 buffer too small")
-    _need_beside(w, codes=codes, scales=scales, row_err=row_err, t2=t2)
+    on = _mx_stream(stream, w, codes, scales, row_err, t2)
     _check(lib().higgs_mx_layer_error(_ptr(w), _dtype_code(w), out, inp, _ptr(codes), _ptr(scales),
-                                      g, seed, _ptr(row_err), _ptr(t2), _stream(stream)))
+                                      g, seed, _ptr(row_err), _ptr(t2), on))
     if stream is not None:
         stream.synchronize()
     return float(t2.item()), row_err
@@ -679,12 +688,12 @@ def mx_qmatmul(x, codes, scales, fmt: int, g: int, seed: int, out_features: int,
     own = workspace is None
     workspace, ws_ptr, ws_bytes = _workspace(
         workspace, _of_sizes(_mx_workspace, batch, out_features, inp, fmt, g), x)
-    _need_beside(x, codes=codes, scales=scales, y=y, workspace=workspace)
-    if own and workspace is not None and stream is not None:
+    on = _mx_stream(stream, x, codes, scales, y, workspace)
+    if stream is not None and own and workspace is not None:
         workspace.record_stream(stream)  # given back to the allocator only after the call's work
     _check(lib().higgs_mx_qmatmul(_ptr(x), _dtype_code(x), batch, fmt, _ptr(codes), _ptr(scales),
                                   g, seed, out_features, inp, _ptr(y), _dtype_code(y), ws_ptr,
-                                  ws_bytes, _stream(stream)))
+                                  ws_bytes, on))
     return y
 
 

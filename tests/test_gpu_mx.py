@@ -645,3 +645,25 @@ def test_linear_captured_beside_an_eager_one(H):
             eager = layer.forward(x)
             torch.cuda.synchronize()
             assert torch.equal(y, w) and torch.equal(eager, w)
+
+
+def test_refuses_another_device(H, monkeypatch):
+    """Tensors of one device on the current stream or a stream of another."""
+    announce("other device")
+    w = torch.zeros((4, 128), device="cuda")
+    codes, scales = H.mx_quantize(w)
+
+    class Elsewhere:
+        device = torch.device("cuda", 1)
+        cuda_stream = 0
+    calls = [lambda s=None: H.mx_quantize(w, stream=s),
+             lambda s=None: H.mx_dequantize(codes, scales, 128, stream=s),
+             lambda s=None: H.mx_layer_error(w, codes, scales, stream=s),
+             lambda s=None: H.mx_qmatmul(w, codes, scales, H.MX_FP6, 0, 0, 4, stream=s)]
+    for call in calls:
+        with pytest.raises(ValueError, match="stream"):
+            call(Elsewhere())
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    for call in calls:
+        with pytest.raises(ValueError, match="stream"):
+            call()
