@@ -143,8 +143,11 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   // one block lie in distinct banks (of 64, two rows)
   static_assert(kWLoads % kWaves == 0 && kWaves % 2 == 0, "row = 8 wave + lane / 8 mod 16");
   const int wunit = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
+  // LDS row 32 (TN w + n) + c holds column TN (32 w + c) + n of the tile: a lane's TN
+  // accumulators of a row are consecutive outputs
   auto row_offset = [&](const Tile& t, int i, int side) MX_INLINE {
-    const int row = (wave + i * kWaves) * 8 + lane / 8 + side * (BN / 2);
+    const int place = (wave + i * kWaves) * 8 + lane / 8 + side * (BN / 2);
+    const int row = place / (32 * TN) * (32 * TN) + place % 32 * TN + place / 32 % TN;
     const int64_t o = min(int64_t(t.nt) * BN + row, a.out - 1);
     // (the second half's first pair begins a stage early: what that reads is not used)
     return uint32_t(o) * uint32_t(a.blocks * 16) + uint32_t(t.first * 64 + wunit * 16 - side * 64);
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
     if constexpr (k >= kReads) {
       constexpr int q = k - kReads;
       const int at = q < TM ? kXScale + ((wm * TM + q) * 32 + r32) * 4
-                            : kWScale + ((wn * TN + q - TM) * 32 + r32) * 4;
+                            : kWScale + ((wn * 32 + r32) * TN + q - TM) * 4;
       words[q] = *reinterpret_cast<const uint32_t*>(s + at);
     } else if constexpr (k >= kXReads && k < kXReads + TN) {
       constexpr int n = k - kXReads;
@@ -366,7 +369,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   auto wrap = [](int v, int n) MX_INLINE { return v == n ? 0 : v; };
   // Stores of whole tiles stay in flight over the first meeting of the next tile: at
   // least that many operations are younger than the loads it waits for.
-  constexpr int kStores = sizeof(OutT) == 4 ? TM * TN * 16 : TM * TN * 8;
+  constexpr int kStores = TM * 16;
   constexpr int kRelaxed = (NB - 2) * kLoads + kStores < 63 ? (NB - 2) * kLoads + kStores : 63;
   bool relaxed = false;
   while (true) {
@@ -397,55 +400,57 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
     }
     at.stage = 0;
 
-    // ---- outputs: register i holds row i % 4 + 8 (i / 4) + 4 hi, column r32 ----
+    // ---- outputs: register i of accumulator n holds row i % 4 + 8 (i / 4) + 4 hi, column
+    //      TN r32 + n ----
     const bool partial = a.splits > 1;
     const int64_t bw = int64_t(now.mt) * BM + wm * TM * 32;
     const int64_t ow = int64_t(now.nt) * BN + wn * TN * 32;
     const int brows = int(min(a.batch - bw, int64_t(BM))) - 4 * hi;
-    const int ocols = int(min(a.out - ow, int64_t(BN))) - r32;
+    const int ocols = int(min(a.out - ow, int64_t(BN))) - TN * r32;
     const bool full = a.batch - bw >= TM * 32 && a.out - ow >= TN * 32;
+    auto each_row = [&](auto f) MX_INLINE {
+#pragma unroll
+      for (int m = 0; m < TM; ++m)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) f(m, i, m * 32 + i % 4 + 8 * (i / 4));
+    };
     if (sizeof(OutT) == 4 || partial) {
+      typedef float run_t __attribute__((ext_vector_type(TN), aligned(4)));
       float* const y = static_cast<float*>(a.y) + (partial ? now.split * a.batch * a.pitch : 0) +
                        bw * a.pitch + ow;
-      const uint32_t lane_at = uint32_t(4 * hi) * uint32_t(a.pitch) + uint32_t(r32);
+      const uint32_t lane_at = uint32_t(4 * hi) * uint32_t(a.pitch) + uint32_t(TN * r32);
+      each_row([&](int m, int i, int b) MX_INLINE {
+        if (full) {
+          run_t v;
 #pragma unroll
-      for (int m = 0; m < TM; ++m)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int b = m * 32 + i % 4 + 8 * (i / 4);
+          for (int n = 0; n < TN; ++n) v[n] = acc[m][n][i];
+          *reinterpret_cast<run_t*>(y + b * a.pitch + lane_at) = v;
+        } else if (b < brows) {
 #pragma unroll
           for (int n = 0; n < TN; ++n)
-            if (full || (b < brows && n * 32 < ocols))
-              y[b * a.pitch + n * 32 + lane_at] = acc[m][n][i];
+            if (n < ocols) y[b * a.pitch + lane_at + n] = acc[m][n][i];
         }
+      });
     } else {
-      // two rows of a column per word; lanes 2 j and 2 j + 1 exchange them to two
-      // columns of a row, lane 2 j storing the first row and lane 2 j + 1 the second
       uint16_t* const y = static_cast<uint16_t*>(a.y) + bw * a.pitch + ow;
-      const int odd = lane & 1;
-      const bool pairs = full && a.pitch % 2 == 0;
-      const uint32_t lane_at = uint32_t(4 * hi + odd) * uint32_t(a.pitch) + uint32_t(r32 - odd);
-      const uint32_t each_at = uint32_t(4 * hi) * uint32_t(a.pitch) + uint32_t(r32);
+      const uint32_t lane_at = uint32_t(4 * hi) * uint32_t(a.pitch) + uint32_t(TN * r32);
+      each_row([&](int m, int i, int b) MX_INLINE {
+        uint32_t v[(TN + 1) / 2];
 #pragma unroll
-      for (int m = 0; m < TM; ++m)
+        for (int n = 0; n < TN; n += 2)
+          v[n / 2] = pack_bf16(acc[m][n][i], n + 1 < TN ? acc[m][n + 1 < TN ? n + 1 : n][i] : 0.f);
+        if (full && TN > 1) {
+          typedef uint32_t run_t __attribute__((ext_vector_type((TN + 1) / 2), aligned(2)));
+          run_t u;
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const int b = m * 32 + i % 4 + 8 * (i / 4);
+          for (int n = 0; n < TN / 2; ++n) u[n] = v[n];
+          *reinterpret_cast<run_t*>(y + b * a.pitch + lane_at) = u;
+        } else if (b < brows) {
 #pragma unroll
-          for (int n = 0; n < TN; ++n) {
-            const uint32_t v = pack_bf16(acc[m][n][i], acc[m][n][i + 1]);
-            if (pairs) {
-              const uint32_t p = lane_xor_small<1>(v);
-              // even: (own low, partner's low); odd: (partner's high, own high)
-              const uint32_t w = odd ? __builtin_amdgcn_perm(v, p, 0x07060302u)
-                                     : __builtin_amdgcn_perm(p, v, 0x05040100u);
-              *reinterpret_cast<uint32_t*>(y + b * a.pitch + n * 32 + lane_at) = w;
-            } else if (n * 32 < ocols) {
-              if (b < brows) y[b * a.pitch + n * 32 + each_at] = uint16_t(v);
-              if (b + 1 < brows) y[(b + 1) * a.pitch + n * 32 + each_at] = uint16_t(v >> 16);
-            }
-          }
+          for (int n = 0; n < TN; ++n)
+            if (n < ocols) y[b * a.pitch + lane_at + n] = uint16_t(v[n / 2] >> (16 * (n & 1)));
         }
+      });
     }
     if (now.item + step >= end) break;
     now = locate(now.item + step);
