@@ -67,8 +67,8 @@ __device__ MX_INLINE inline void for_each(const F& f) {
 // activations, weights and scale words go from memory to LDS, from there into the
 // operands. The loads run NB - 1/2 stages ahead. Weights are loaded for two stages at
 // a time, 128 bytes of a row: the address unit takes about as long for half a line as
-// for a whole one (62, 88 and 106 GB/s per compute unit in pieces of 64, 128 and 256 bytes), and
-// that time is what the products have to hide. So that every stage loads as much,
+// for a whole one (62, 88 and 106 GB/s per compute unit in pieces of 64, 128 and 256
+// bytes), and that time is what the products have to hide. So that every stage loads as much,
 // the block's first half of columns has its pairs of stages at (0, 1), (2, 3) ..,
 // the second at (-1, 0), (1, 2) .. (NB is odd; a range of K has an even number of
 // stages). The loads run on into the next tile, so that its first stages arrive while
@@ -102,8 +102,9 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   const int wm = wave % WM, wn = wave / WM;
   const int r32 = lane & 31, hi = lane >> 5;
 
-  // ---- the block's tiles: consecutive ones per XCD, dealt to its blocks in turn; eight
-  //      row tiles of one column after another (their weights stay in the XCD's L2) ----
+  // ---- the block's tiles: consecutive ones per XCD, dealt to its blocks in turn; four
+  //      row tiles of one column after another (their weights stay in the XCD's L2; 2048 x
+  //      4096 -> 28672 takes 167 us with four, 171 with two, 176 with eight) ----
   const int total = a.mtiles * a.ntiles * a.splits;
   const int xcd = int(blockIdx.x) % 8, step = (int(gridDim.x) + 7) / 8;  // (its blocks)
   const int end = (xcd + 1) * (total / 8) + min(xcd + 1, total % 8);
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
     r.item = item;
     r.split = uniform(item / (a.mtiles * a.ntiles));
     const int tile = item - r.split * (a.mtiles * a.ntiles);
-    constexpr int kBand = 8;
+    constexpr int kBand = 4;
     const int band = uniform(tile / (kBand * a.ntiles)), rest = tile - band * (kBand * a.ntiles);
     const int high = min(kBand, a.mtiles - band * kBand);
     r.nt = uniform(rest / high);
@@ -614,10 +615,13 @@ template <int FMT, typename OutT>
 hipError_t launch_shape(int shape, Args a, hipStream_t stream) {
   a.mtiles = int((a.batch + kShapes[shape].bm - 1) / kShapes[shape].bm);
   a.ntiles = int((a.out + kShapes[shape].bn - 1) / kShapes[shape].bn);
+  // (4-bit activations leave room for five stages of two blocks of 64 x 128: 19.0 us for 200
+  // x 4096 -> 8192, 21.9 with three; 128 x 256 gains nothing from five)
   switch (shape) {
     case 0: return launch_tiles<256, 256, 4, 2, 3, 1, FMT, OutT>(a, stream);
     case 1: return launch_tiles<128, 128, 2, 2, 3, 2, FMT, OutT>(a, stream);
-    case 2: return launch_tiles<64, 128, 2, 2, 3, 2, FMT, OutT>(a, stream);
+    case 2:
+      return launch_tiles<64, 128, 2, 2, FMT == HIGGS_MX_FP4 ? 5 : 3, 2, FMT, OutT>(a, stream);
     case 3: return launch_tiles<32, 128, 1, 4, 5, 2, FMT, OutT>(a, stream);
     default: return launch_tiles<128, 256, 2, 4, 3, 1, FMT, OutT>(a, stream);
   }
