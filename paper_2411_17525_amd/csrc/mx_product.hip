@@ -8,8 +8,7 @@
 // Operands of v_mfma_scale_f32_32x32x64_f8f6f4 (either format): lane l holds
 // the block l / 32 of two (32 consecutive values of K) of row l % 32 and its
 // scale byte; of the result it holds column l % 32, rows i % 4 + 8 (i / 4) +
-// 4 (l / 32). The activations are the rows, the weights the columns: a store of
-// one register then writes 32 consecutive outputs.
+// 4 (l / 32). The activations are the rows, the weights the columns.
 
 #include <algorithm>
 

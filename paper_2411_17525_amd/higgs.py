@@ -586,6 +586,8 @@ def _need_mx_layer(codes, scales, rows, inp, fmt):
     cb, sb = _of_sizes(_mx_row_bytes, inp, fmt)
     if codes.numel() < rows * cb or scales.numel() < rows * sb:
         raise ValueError(f"codes or scales too small for {rows} rows of {inp}")
+    if codes.dim() == 2 and codes.shape[1] != cb or scales.dim() == 2 and scales.shape[1] != sb:
+        raise ValueError(f"codes or scales of rows of another length than {inp}")
 
 
 def _mx_dtype(dtype):

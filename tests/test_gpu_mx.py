@@ -667,3 +667,25 @@ def test_refuses_another_device(H, monkeypatch):
     for call in calls:
         with pytest.raises(ValueError, match="stream"):
             call()
+
+
+def test_refuses_rows_of_another_length(H):
+    announce("row length")
+    x = torch.zeros((4, 64), device="cuda")
+    codes, scales = H.mx_quantize(torch.zeros((4, 128), device="cuda"))
+    for call in (lambda: H.mx_dequantize(codes, scales, 64),
+                 lambda: H.mx_layer_error(x, codes, scales),
+                 lambda: H.mx_qmatmul(x, codes, scales, H.MX_FP6, 0, 0, 4),
+                 lambda: H.mx_quantize(x, codes=codes), lambda: H.mx_quantize(x, scales=scales)):
+        with pytest.raises(ValueError, match="another length"):
+            call()
+    # buffers without rows, and with more of them, are taken
+    flat = H.mx_dequantize(codes, scales.view(-1), 128)
+    assert flat.shape == (4, 128) and not flat.any()
+    y = H.mx_qmatmul(x[:1].repeat(1, 2), codes.view(-1), scales.view(-1), H.MX_FP6, 0, 0, 3)
+    assert y.shape == (1, 3) and not y.any()
+
+
+@pytest.mark.parametrize("batch,g", [(1, 4096), (16, 0), (32, 1024), (40, 0)])
+def test_product_of_the_longest_rows(H, batch, g):
+    check_product(H, batch, 24, 1 << 20, "fp6", g, "bf16", "f32")
