@@ -34,7 +34,7 @@ struct Args {
   int64_t pitch;  // of a row of y and of ws, in values: out, or more for a part of the outputs
   int blocks;  // of a weight row
   int splits;  // of K
-  int mtiles, ntiles;
+  int mtiles, ntiles, band;
 };
 
 template <int N>
@@ -101,9 +101,8 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   const int wm = wave % WM, wn = wave / WM;
   const int r32 = lane & 31, hi = lane >> 5;
 
-  // ---- the block's tiles: consecutive ones per XCD, dealt to its blocks in turn; four
-  //      row tiles of one column after another (their weights stay in the XCD's L2; 2048 x
-  //      4096 -> 28672 takes 167 us with four, 171 with two, 176 with eight) ----
+  // ---- the block's tiles: consecutive ones per XCD, dealt to its blocks in turn; a band
+  //      of row tiles of one column after another (their weights stay in the XCD's L2) ----
   const int total = a.mtiles * a.ntiles * a.splits;
   const int xcd = int(blockIdx.x) % 8, step = (int(gridDim.x) + 7) / 8;  // (its blocks)
   const int end = (xcd + 1) * (total / 8) + min(xcd + 1, total % 8);
@@ -117,11 +116,10 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
     r.item = item;
     r.split = uniform(item / (a.mtiles * a.ntiles));
     const int tile = item - r.split * (a.mtiles * a.ntiles);
-    constexpr int kBand = 4;
-    const int band = uniform(tile / (kBand * a.ntiles)), rest = tile - band * (kBand * a.ntiles);
-    const int high = min(kBand, a.mtiles - band * kBand);
+    const int band = uniform(tile / (a.band * a.ntiles)), rest = tile - band * (a.band * a.ntiles);
+    const int high = min(a.band, a.mtiles - band * a.band);
     r.nt = uniform(rest / high);
-    r.mt = band * kBand + rest - r.nt * high;
+    r.mt = band * a.band + rest - r.nt * high;
     r.first = uniform(stages / 2 * r.split / a.splits) * 2;
     r.count = uniform(stages / 2 * (r.split + 1) / a.splits) * 2 - r.first;
     return r;
@@ -257,15 +255,21 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   // read k of a half's operands, in the order in which the products need them: the
   // first row tile, all column tiles, the other row tiles; then the scale words
   constexpr int kXReads = FMT == HIGGS_MX_FP6 ? 2 : 1;
-  constexpr int kReads = TM * kXReads + TN;
+  constexpr int kReads = TM * kXReads + TN, kScaleReads = TM + 1;
   auto read = [&](auto K, Half& f, int t, int buf, int pair0, int pair1, int h) MX_INLINE {
     constexpr int k = decltype(K)::value;
     const uint8_t* const s = s_mem + buf * kStage;
     if constexpr (k >= kReads) {
       constexpr int q = k - kReads;
-      const int at = q < TM ? kXScale + ((wm * TM + q) * 32 + r32) * 4
-                            : kWScale + ((wn * 32 + r32) * TN + q - TM) * 4;
-      words[q] = *reinterpret_cast<const uint32_t*>(s + at);
+      if constexpr (q < TM) {
+        words[q] =
+            *reinterpret_cast<const uint32_t*>(s + kXScale + ((wm * TM + q) * 32 + r32) * 4);
+      } else {
+        typedef uint32_t run_t __attribute__((ext_vector_type(TN)));
+        const run_t u = *reinterpret_cast<const run_t*>(s + kWScale + (wn * 32 + r32) * TN * 4);
+#pragma unroll
+        for (int n = 0; n < TN; ++n) words[TM + n] = u[n];
+      }
     } else if constexpr (k >= kXReads && k < kXReads + TN) {
       constexpr int n = k - kXReads;
       const int row = (wn * TN + n) * 32 + r32;
@@ -323,7 +327,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
                   int lside, int lbuf, int lpair) MX_INLINE {
     constexpr int kOver = kProducts >= 4 ? kProducts * 3 / 4 : kProducts;
     constexpr int l0 = decltype(L0)::value, nl = decltype(L1)::value - l0;
-    constexpr int kAll = kReads + (decltype(H)::value == 1 ? TM + TN : 0);
+    constexpr int kAll = kReads + (decltype(H)::value == 1 ? kScaleReads : 0);
     for_each<kProducts>([&](auto I) MX_INLINE {
       constexpr int i = decltype(I)::value;
       multiply(I, now, H);
@@ -361,7 +365,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PERCU / 4) void mx_product_
   wait_vm<(NB - 2) * kLoads + LH::value>();
   wait_lds_and_meet();
   Half f0, f1;
-  for_each<kReads + TM + TN>([&](auto K) MX_INLINE { read(K, f0, 0, 0, 0, 0, 0); });
+  for_each<kReads + kScaleReads>([&](auto K) MX_INLINE { read(K, f0, 0, 0, 0, 0, 0); });
   // lpair: the pair buffer of the loads for stage t + NB - 1; pair0, pair1: those of
   // stage t. A pair's buffer is taken up two stages later by the pair kPairs on.
   Place at{0, 0, 0, 0};
@@ -501,8 +505,8 @@ int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 // stage's share of its compute unit where that is what bounds it, the start and the
 // outputs of a tile. Fitted to 2500 calls of 20 .. 2048 rows and nine layers (outputs
 // x K from 512 x 512 to 28672 x 4096), each under every shape and 1 .. 8 splits: the
-// plan that is fastest by these numbers took 0.4% longer than the fastest measured
-// one on average, 8% at most.
+// plan that is fastest by these numbers takes 0.7% longer than the fastest measured
+// one on average, 11% at most.
 struct Shape {
   int bm, bn, percu;
   double latency, share, tile;
@@ -614,6 +618,10 @@ template <int FMT, typename OutT>
 hipError_t launch_shape(int shape, Args a, hipStream_t stream) {
   a.mtiles = int((a.batch + kShapes[shape].bm - 1) / kShapes[shape].bm);
   a.ntiles = int((a.out + kShapes[shape].bn - 1) / kShapes[shape].bn);
+  // bands of equal height near four (2048 x 4096 -> 28672 takes 167 us with four row tiles,
+  // 171 with two, 176 with eight), up to six in one
+  const int bands = std::max(1, (a.mtiles + 1) / 4);
+  a.band = (a.mtiles + bands - 1) / bands;
   // (4-bit activations leave room for five stages of two blocks of 64 x 128: 19.0 us for 200
   // x 4096 -> 8192, 21.9 with three; 128 x 256 gains nothing from five)
   switch (shape) {
