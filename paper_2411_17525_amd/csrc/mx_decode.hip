@@ -30,9 +30,18 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int kMaxWaves = 8;
-// Values that a block converts itself: above that the conversion takes longer than
-// the launch that it saves.
+// Values that a block converts itself; with a rotation at most 14 segments of 1024, two
+// per wave. Above that the conversion takes longer than the launch that it saves (3 x 4096
+// -> 4096 8.4 us fused and 8.8 not, 4 x 4096 9.5 and 8.9; with two waves, 4 x 1024 -> 1024
+// 5.7 and 6.3, 16 x 1024 13.5 and 6.7).
 constexpr int kFusedValues = 16384;
+constexpr int kFusedSegments = 14;
+
+// As few waves as take equal shares of a row's chunks in as many turns as the most would.
+int waves_of(int64_t in) {
+  const int64_t chunks = (in + 511) / 512, turns = (chunks + kMaxWaves - 1) / kMaxWaves;
+  return int((chunks + turns - 1) / turns);
+}
 
 struct Args {
   const void* x;  // FUSED: raw activations
@@ -177,7 +186,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
         const int left = a.in - 1024 * seg;
         double v[16];
         if (a.x_bf16)
-          signed_pairs(load_pairs(static_cast<const uint16_t*>(a.x) + at, left, lane), neg.of(0), v);
+          signed_pairs(load_pairs(static_cast<const uint16_t*>(a.x) + at, left, lane), neg.of(0),
+                       v);
         else
           signed_pairs(load_pairs(static_cast<const float*>(a.x) + at, left, lane), neg.of(0), v);
         uint32_t c[kWords16<FMT>], byte;
@@ -216,7 +226,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
     if constexpr (kFused) {
       const int at = (4 * t + q) * batch + min(r16, batch - 1);
       u = *reinterpret_cast<const u32x4*>(s_mem + kX + at * 16);
-      if constexpr (FMT == HIGGS_MX_FP6) v = *reinterpret_cast<const u32x2*>(s_mem + kXTail + at * 8);
+      if constexpr (FMT == HIGGS_MX_FP6)
+        v = *reinterpret_cast<const u32x2*>(s_mem + kXTail + at * 8);
       s = *reinterpret_cast<const uint32_t*>(s_mem + kXScale + (t * batch + min(r16, batch - 1)) * 4);
     } else {
       const uint8_t* const p = a.t.codes + (t * 2 + (q >> 1)) * mx_half_bytes(FMT);
@@ -305,15 +316,12 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
 
 template <int FMT, int G, int NT>
 hipError_t launch(const Args& a, hipStream_t stream) {
-  // as few waves as take equal shares of the chunks in as many turns as the most would
-  const int turns = (a.chunks + kMaxWaves - 1) / kMaxWaves;
-  const int waves = (a.chunks + turns - 1) / turns;
   // as many blocks as the compute units hold, or fewer: two each, one where the
   // activations are in LDS too or with two tiles of them (16 x 4096 -> 28672 with 256
   // blocks instead of 512: 21.3 us, not 18.7)
   constexpr int kBlocks = G < 0 && NT == 1 ? 512 : 256;
   hipLaunchKernelGGL((mx_decode<FMT, G, NT>), dim3(unsigned(std::min(a.tiles, kBlocks))),
-                     dim3(unsigned(64 * waves)), 0, stream, a);
+                     dim3(unsigned(64 * waves_of(a.in))), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -335,7 +343,9 @@ hipError_t launch_fmt(const Args& a, bool fused, int g, hipStream_t stream) {
 }  // namespace
 
 bool mx_decode_fuses(int64_t batch, int64_t in, int g) {
-  return batch <= 16 && g <= 1024 && batch * in <= kFusedValues;
+  if (batch > 16 || g > 1024 || batch * in > kFusedValues) return false;
+  const int64_t segments = batch * ((in + 1023) / 1024);
+  return g == 0 || (segments <= kFusedSegments && segments <= 2 * waves_of(in));
 }
 
 hipError_t launch_mx_decode(const void* x, higgs_dtype x_dtype, int64_t batch, int fmt,
