@@ -689,3 +689,14 @@ def test_refuses_rows_of_another_length(H):
 @pytest.mark.parametrize("batch,g", [(1, 4096), (16, 0), (32, 1024), (40, 0)])
 def test_product_of_the_longest_rows(H, batch, g):
     check_product(H, batch, 24, 1 << 20, "fp6", g, "bf16", "f32")
+
+
+@pytest.mark.parametrize("batch,inp,g", [
+    (2, 4096, 1024), (3, 4096, 64), (4, 4096, 256), (1, 14336, 2048), (1, 14336, 512), (1, 15360, 1024),
+    (4, 1024, 128), (5, 1024, 1024), (14, 1024, 64), (2, 7168, 1024), (4, 4096, 0), (5, 4096, 0),
+    (16, 1024, 0), (16, 1088, 64)])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_product_of_few_rows(H, batch, inp, g, fmt):
+    """Calls on both sides of where the product converts its activations itself."""
+    for out, x_type in ((50, "bf16"), (4100, "f32")):
+        check_product(H, batch, out, inp, fmt, g, x_type, "f32")
