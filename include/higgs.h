@@ -511,7 +511,9 @@ higgs_status higgs_mx_quantize(const void *W, higgs_dtype w_dtype, int64_t rows,
 /* higgs_mx_dequantize - codes and scales to W [rows][in] of w_dtype. With
  * g = 0 the stored values (of rotated rows: in the rotated space); with the g
  * and rht_seed of the quantization the values rotated back,
- * sigma * H(values) / sqrt(g) per group. Device, asynchronous, one launch.
+ * sigma * H(values) / sqrt(g) per group, summed in fp32 with room for every
+ * value: infinite only where the result exceeds w_dtype. Device, asynchronous,
+ * one launch.
  *   codes   [in]  device, 16-byte aligned; any codes and scale bytes.
  *   W       [out] device, rows*in values, 16-byte aligned.
  * Requirements as for higgs_mx_quantize. */

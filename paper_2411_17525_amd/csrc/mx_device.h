@@ -34,9 +34,10 @@ __device__ inline void mx_butterflies(T (&v)[16]) {
     }
 }
 
-// H per group, from pairs to runs, or (BACK) from runs to pairs. Pair p is at p + 8 (p
-// / 64) of the scratch between pairs and the middle order, at p + p / 8 between that
-// and runs: both sides of both reach distinct banks.
+// H per group, from pairs to runs, or (BACK) from runs to pairs, there without the
+// butterflies of bit 0, which are the caller's. Pair p is at p + 8 (p / 64) of the scratch
+// between pairs and the middle order, at p + p / 8 between that and runs: both sides of
+// both reach distinct banks.
 template <int G, bool BACK, typename T>
 __device__ inline void mx_fwht(T (&v)[16], uint32_t* scratch, int lane) {
   static_assert(G == 64 || G == 128 || G == 256 || G == 512 || G == 1024, "group size");
@@ -74,7 +75,6 @@ __device__ inline void mx_fwht(T (&v)[16], uint32_t* scratch, int lane) {
     write(pairs, 72);
     read(middle, 8);
   } else {
-    mx_butterflies<1>(v);
     low();
     write(runs, 1);
     read(middle, 9);

@@ -243,12 +243,39 @@ __global__ __launch_bounds__(256) void mx_quantize_plain(const InT* __restrict__
 
 // ---- the way back ----
 
+// Values are rotated back times 2^-16: sums of 4096 of the largest, 7.5 * 2^127, stay in
+// fp32's range, so that only results beyond it are infinite, and multiples of 2^-146
+// (steps of 2^-3 in blocks of the smallest exponent, -127) are still exact in it. The
+// shift is part of the power of two that the decoding multiplies by; what scale bytes
+// below 16 cannot hold of it, the first butterflies multiply by (both values of each are
+// of one block; exact).
+constexpr uint32_t kBackShift = 16;
+template <int FMT>
+__device__ inline void mx_decode16_back(const uint32_t* c, uint32_t byte, float (&v)[16]) {
+  const uint32_t part = min(byte, kBackShift);
+  mx_decode16<FMT>(c, byte == 255 ? 255 : byte - part, v);
+  const float rest = __builtin_bit_cast(float, (127 - kBackShift + part) << 23);
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) {
+    const float x = v[i] * rest, y = v[i + 1];
+    v[i] = __builtin_fmaf(y, rest, x);
+    v[i + 1] = __builtin_fmaf(-y, rest, x);
+  }
+}
+
+// 2^16 / sqrt(G) as a float and, where it is no power of two, the rest of it: the product
+// with both is rounded once (by the rounded factor alone fp32 results of G = 128, 512 and
+// 2048 are off by up to a whole step).
+struct MxBackRoot {
+  float high, low;
+};
+
 // Rotated back in fp32 (stored values are not decided at borders): codes of 16
 // consecutive values per lane, values stored as pairs.
 template <int G, int FMT, typename OutT>
 __global__ __launch_bounds__(64 * kWaves, kRotationWaves<G>) void mx_dequantize_rht(
     const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t total,
-    const MxSigns signs, float root, OutT* __restrict__ w) {
+    const MxSigns signs, const MxBackRoot root, OutT* __restrict__ w) {
   constexpr int S = kSegments<G>;
   __shared__ __attribute__((aligned(16))) uint32_t s_lds[kWaves][kMxWaveLds<float>];
   const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
@@ -264,7 +291,7 @@ __global__ __launch_bounds__(64 * kWaves, kRotationWaves<G>) void mx_dequantize_
         load_codes16<FMT>(codes + (at / 16) * (4 * kWords16<FMT>), c);
         byte = scales[at / 32];
       }
-      mx_decode16<FMT>(c, byte, x[s]);
+      mx_decode16_back<FMT>(c, byte, x[s]);
     }
 #pragma unroll
     for (int s = 0; s < S; ++s) mx_fwht<G < 1024 ? G : 1024, true>(x[s], s_lds[wave], lane);
@@ -272,7 +299,9 @@ __global__ __launch_bounds__(64 * kWaves, kRotationWaves<G>) void mx_dequantize_
 #pragma unroll
     for (int s = 0; s < S; ++s) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[s][i] *= root;
+      for (int i = 0; i < 16; ++i)
+        x[s][i] = kRootShift<G> != 0 ? x[s][i] * root.high
+                                     : __builtin_fmaf(x[s][i], root.high, x[s][i] * root.low);
       store_pairs(w + k + 1024 * s, S > 1 ? 1024 : total - k, neg.of(s), lane, x[s]);
     }
   }
@@ -524,7 +553,8 @@ hipError_t dequantize_typed(const uint8_t* codes, const uint8_t* scales, int64_t
   }
   MxSigns signs;
   mx_signs(seed, g, &signs);
-  const float root = float(1.0 / std::sqrt(double(g)));
+  const double factor = std::ldexp(1.0 / std::sqrt(double(g)), kBackShift);
+  const MxBackRoot root{float(factor), float(factor - double(float(factor)))};
   const int64_t total = rows * in;
   for_group(g, [&](auto G) {
     constexpr int kG = decltype(G)::value;
