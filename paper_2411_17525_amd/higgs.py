@@ -546,6 +546,10 @@ def qmatmul_fused_multi(x, layers, grid, g: int, ys=None, workspace=None, stream
 
 # ---------------------------------------------------------------------------
 # microscaled layers (blocks of 32 values with one power of two each)
+#
+# Device calls run on the current stream or, with `stream`, on that one: it is the
+# caller who orders it behind the work that makes the tensors passed in, who keeps these
+# until its work has ended, and who orders the results' use behind it.
 # ---------------------------------------------------------------------------
 
 def mx_codes_row_bytes(inp: int, fmt: int = MX_FP4) -> int:
@@ -567,17 +571,33 @@ def _need_matrix(name, t, dtypes):
         raise ValueError(f"{name} must have two dimensions")
 
 
-def _mx_stream(stream, first, *tensors):
-    """The call's stream (the current one), which is to be on the device of all tensors."""
+def _mx_call_on(stream, call, first, *args):
+    """call(first, *args) with `stream` current, so that what it allocates is that stream's
+    memory: a block from the current stream's may still be in use by work queued there.
+    New results are for the current stream as well: their memory is not handed out again
+    before the work that it holds when they are released."""
+    if isinstance(first, _torch.Tensor) and first.get_device() != stream.device.index:
+        raise ValueError(f"tensors on {first.device}, stream on {stream.device}")
+    here = _torch.cuda.current_stream(stream.device)
+    with _torch.cuda.stream(stream):
+        results = call(first, *args)
+    for t in results if isinstance(results, tuple) else (results,):
+        if isinstance(t, _torch.Tensor) and not any(t is a for a in args):
+            t.record_stream(here)
+    return results
+
+
+def _mx_stream(first, *tensors):
+    """The current stream, which is to be on the device of all tensors."""
     device = first.get_device()
     for t in tensors:
         if t is not None and t.get_device() != device:
             raise ValueError(f"tensors on {first.device} and {t.device}")
     cuda = _torch._C
-    on = cuda._cuda_getDevice() if stream is None else stream.device.index
+    on = cuda._cuda_getDevice()
     if on != device:
         raise ValueError(f"tensors on {first.device}, stream on cuda:{on}")
-    return cuda._cuda_getCurrentRawStream(on) if stream is None else int(stream.cuda_stream)
+    return cuda._cuda_getCurrentRawStream(on)
 
 
 def _need_mx_layer(codes, scales, rows, inp, fmt):
@@ -613,6 +633,8 @@ def mx_quantize(w, fmt: int = MX_FP4, g: int = 0, seed: int = 0, codes=None, sca
 
     Returns (codes uint8 [rows, row_bytes], scales uint8 [rows, ceil(in/32)])."""
     _need_torch()
+    if stream is not None:
+        return _mx_call_on(stream, mx_quantize, w, fmt, g, seed, codes, scales)
     _need_matrix("w", w, _FLOATS)
     rows, inp = w.shape
     cb, sb = _of_sizes(_mx_row_bytes, inp, fmt)
@@ -621,7 +643,7 @@ def mx_quantize(w, fmt: int = MX_FP4, g: int = 0, seed: int = 0, codes=None, sca
     codes = _new(w, rows, cb, _torch.uint8) if codes is None else codes
     scales = _new(w, rows, sb, _torch.uint8) if scales is None else scales
     _need_mx_layer(codes, scales, rows, inp, fmt)
-    on = _mx_stream(stream, w, codes, scales)
+    on = _mx_stream(w, codes, scales)
     _check(lib().higgs_mx_quantize(_ptr(w), _dtype_code(w), rows, inp, fmt, g, seed, _ptr(codes),
                                    _ptr(scales), on))
     return codes, scales
@@ -632,6 +654,9 @@ def mx_dequantize(codes, scales, in_features: int, fmt: int = MX_FP4, g: int = 0
     """The stored values [rows, in_features] (g = 0), or rotated back to the original
     space (g and seed as quantized), in float32 (default) or bfloat16."""
     _need_torch()
+    if stream is not None:
+        return _mx_call_on(stream, mx_dequantize, codes, scales, in_features, fmt, g, seed, dtype,
+                           out)
     _need_matrix("codes", codes, _U8)
     rows = codes.shape[0]
     dtype = _mx_dtype(out.dtype if dtype is None and out is not None else dtype)
@@ -641,7 +666,7 @@ def mx_dequantize(codes, scales, in_features: int, fmt: int = MX_FP4, g: int = 0
     _need_cuda("out", out, (dtype,))
     if out.numel() < rows * in_features:
         raise ValueError("out buffer too small")
-    on = _mx_stream(stream, codes, scales, out)
+    on = _mx_stream(codes, scales, out)
     _check(lib().higgs_mx_dequantize(_ptr(codes), _ptr(scales), rows, in_features, fmt, g, seed,
                                      _ptr(out), _dtype_code(out), on))
     return out
@@ -653,6 +678,8 @@ def mx_layer_error(w, codes, scales, g: int = 0, seed: int = 0, row_err=None, t2
     tensors [out, 2] and [1]). Returns (t2 as a float, row_err); reading t2
     synchronises the stream."""
     _need_torch()
+    if stream is not None:
+        return _mx_call_on(stream, mx_layer_error, w, codes, scales, g, seed, row_err, t2)
     _need_matrix("w", w, _FLOATS)
     out, inp = w.shape
     _need_mx_layer(codes, scales, out, inp, MX_FP4)
@@ -663,11 +690,9 @@ def mx_layer_error(w, codes, scales, g: int = 0, seed: int = 0, row_err=None, t2
     _need_cuda("t2", t2, f64)
     if row_err.numel() < 2 * out or t2.numel() < 1:
         raise ValueError("row_err or t2 buffer too small")
-    on = _mx_stream(stream, w, codes, scales, row_err, t2)
+    on = _mx_stream(w, codes, scales, row_err, t2)
     _check(lib().higgs_mx_layer_error(_ptr(w), _dtype_code(w), out, inp, _ptr(codes), _ptr(scales),
                                       g, seed, _ptr(row_err), _ptr(t2), on))
-    if stream is not None:
-        stream.synchronize()
     return float(t2.item()), row_err
 
 
@@ -677,6 +702,9 @@ def mx_qmatmul(x, codes, scales, fmt: int, g: int, seed: int, out_features: int,
     or bfloat16, which the call rotates (g > 0) and converts to fmt (MX_FP6 or MX_FP4).
     y is float32 (default) or bfloat16."""
     _need_torch()
+    if stream is not None:
+        return _mx_call_on(stream, mx_qmatmul, x, codes, scales, fmt, g, seed, out_features, y,
+                           workspace, dtype)
     _need_matrix("x", x, _FLOATS)
     batch, inp = x.shape
     _need_mx_layer(codes, scales, out_features, inp, MX_FP4)
@@ -687,12 +715,9 @@ def mx_qmatmul(x, codes, scales, fmt: int, g: int, seed: int, out_features: int,
         _need_cuda("y", y, (dtype,))
         if y.numel() < batch * out_features:
             raise ValueError("y buffer too small")
-    own = workspace is None
     workspace, ws_ptr, ws_bytes = _workspace(
         workspace, _of_sizes(_mx_workspace, batch, out_features, inp, fmt, g), x)
-    on = _mx_stream(stream, x, codes, scales, y, workspace)
-    if stream is not None and own and workspace is not None:
-        workspace.record_stream(stream)  # given back to the allocator only after the call's work
+    on = _mx_stream(x, codes, scales, y, workspace)
     _check(lib().higgs_mx_qmatmul(_ptr(x), _dtype_code(x), batch, fmt, _ptr(codes), _ptr(scales),
                                   g, seed, out_features, inp, _ptr(y), _dtype_code(y), ws_ptr,
                                   ws_bytes, on))
