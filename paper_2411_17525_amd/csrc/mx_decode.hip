@@ -145,6 +145,9 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx_decode(const Args a) {
   auto request = [&](Item& f, int slot) {
     if (next.tile < a.tiles) {
       issue(next.tile, wave + next.k * waves, slot);
+      // (the order that the waits rest on: no scale load is moved before these)
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
       load_scales(next.tile, wave + next.k * waves, f.ws);
     }
   };
