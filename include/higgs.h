@@ -529,7 +529,9 @@ higgs_status higgs_mx_dequantize(const uint8_t *codes, const uint8_t *scales, in
  *   t2       [out] device, nullable, one double: the ratio of their totals (0
  *            for an all-zero layer).
  * Other arguments as for higgs_mx_quantize. W must hold finite values (others
- * make the row's error and t2 NaN or infinite). Requires out < 2^24. */
+ * make the row's error and t2 NaN or infinite); codes that stand for 2^128 or
+ * more (scale bytes 253 and 254; higgs_mx_quantize stores none) count as
+ * infinite. Requires out < 2^24. */
 higgs_status higgs_mx_layer_error(const void *W, higgs_dtype w_dtype, int64_t out, int64_t in,
                                   const uint8_t *codes, const uint8_t *scales, int g,
                                   uint64_t rht_seed, double *row_err, double *t2, void *stream);

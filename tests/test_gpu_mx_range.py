@@ -128,3 +128,27 @@ def test_nan_stays_in_its_group(H, g, fmt):
     clean = scales.copy()
     clean[1, (2 * g + g // 2) // 32] = 0
     assert np.array_equal(got[~nan], back(H, packed, clean, inp, fmt, g, 5, "f32")[~nan])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("batch", [1, 9, 24, 80, 300])
+@pytest.mark.parametrize("x_power,lo,hi", [(-110, 225, 255), (110, 0, 16), (0, 100, 140),
+                                           (-60, 40, 68)])
+def test_product_over_the_range(H, batch, fmt, x_power, lo, hi):
+    """Weights of the largest and the smallest scale bytes with activations that bring the
+    products back into fp32's range, and sums just above its smallest normal value."""
+    announce(f"product batch={batch} x 2^{x_power} bytes {lo}..{hi} {fmt}")
+    out, inp = 70, 1088
+    rng = np.random.default_rng(batch + lo)
+    x = np.ldexp(rng.standard_normal((batch, inp)), x_power).astype(np.float32)
+    packed = rng.integers(0, 256, (out, M.row_bytes(inp, "fp4")), dtype=np.uint8)
+    scales = rng.integers(lo, hi, (out, M.blocks(inp)), dtype=np.uint8)
+    y = H.mx_qmatmul(torch.from_numpy(x).cuda(), torch.from_numpy(packed).cuda(),
+                     torch.from_numpy(scales).cuda(), H.MX_FP4 if fmt == "fp4" else H.MX_FP6, 0, 0,
+                     out).double().cpu().numpy()
+    xq = M.quantized(x.astype(np.float64), fmt)
+    wq = M.values(M.unpack(packed, "fp4"), scales, "fp4", inp)
+    want, size = xq @ wq.T, np.abs(xq) @ np.abs(wq).T
+    # exact products; one rounding of a partial sum per 64 of K, one per part (at most 16)
+    tol = (-(-inp // 64) + 16) * 2.0 ** -24 * size
+    assert (np.abs(y - want) <= tol).all()
