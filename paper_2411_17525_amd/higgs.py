@@ -717,6 +717,8 @@ def mx_qmatmul(x, codes, scales, fmt: int, g: int, seed: int, out_features: int,
             raise ValueError("y buffer too small")
     workspace, ws_ptr, ws_bytes = _workspace(
         workspace, _of_sizes(_mx_workspace, batch, out_features, inp, fmt, g), x)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     on = _mx_stream(x, codes, scales, y, workspace)
     _check(lib().higgs_mx_qmatmul(_ptr(x), _dtype_code(x), batch, fmt, _ptr(codes), _ptr(scales),
                                   g, seed, out_features, inp, _ptr(y), _dtype_code(y), ws_ptr,
