@@ -144,6 +144,26 @@ def _stream(stream):
     return int(stream.cuda_stream)
 
 
+def _call_on(stream, call, *args):
+    """call(*args) with `stream` current, so that what it allocates is that stream's
+    memory: a block from the current stream's may still be in use by work queued there.
+    New results are for the current stream as well: their memory is not handed out again
+    before the work that it holds when they are released."""
+    here = _torch.cuda.current_stream(stream.device)
+    with _torch.cuda.stream(stream):
+        results = call(*args)
+    for t in results if isinstance(results, (tuple, list)) else (results,):
+        if isinstance(t, _torch.Tensor) and not any(t is a for a in args):
+            t.record_stream(here)
+    return results
+
+
+def _is_stream(stream):
+    """A stream to run a whole call on. (Any other object with a cuda_stream is the
+    caller's way to name one for the kernels alone: buffers are to be passed with it.)"""
+    return isinstance(stream, _need_torch().cuda.Stream)
+
+
 def _need_cuda(name, t, dtypes):
     if not isinstance(t, _need_torch().Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
@@ -290,6 +310,8 @@ def search_index(grid, index=None, stream=None):
     every quantize() call that uses that grid.
     """
     import torch
+    if stream is not None and _is_stream(stream):
+        return _call_on(stream, search_index, grid, index)
     _need_cuda("grid", grid, (torch.float32,))
     n, p = grid.shape
     nb = search_index_bytes(p, n)
@@ -310,6 +332,8 @@ def quantize(w, grid, g: int, seed: int, codes=None, scales=None, stream=None, i
     Returns (codes uint8 [out, row_bytes], scales float16 [out, in/g]).
     """
     import torch
+    if stream is not None and _is_stream(stream):
+        return _call_on(stream, quantize, w, grid, g, seed, codes, scales, None, index)
     _need_cuda("w", w, (torch.float32, torch.bfloat16))
     _need_cuda("grid", grid, (torch.float32,))
     out, inp = w.shape
@@ -343,6 +367,8 @@ def layer_error(w, codes, scales, grid, g: int, seed: int, group_err=None, t2=No
     (fp64 device tensors [out * in/g, 2] and [1]). Returns (t2 as a float,
     group_err); reading t2 synchronises the stream."""
     import torch
+    if stream is not None and _is_stream(stream):
+        return _call_on(stream, layer_error, w, codes, scales, grid, g, seed, group_err, t2)
     _need_cuda("w", w, (torch.float32, torch.bfloat16))
     _need_cuda("grid", grid, (torch.float32,))
     _need_cuda("codes", codes, (torch.uint8,))
@@ -387,6 +413,8 @@ def gptq_factor(x_rot, damp: float = 0.01, factor=None, stream=None):
     """U (upper, row-major in a [in, in] float64 tensor) with (H + damping)^-1 =
     U^T U, H = x_rot^T x_rot over rotated calibration activations [samples, in]."""
     import torch
+    if stream is not None and _is_stream(stream):
+        return _call_on(stream, gptq_factor, x_rot, damp, factor)
     _need_cuda("x_rot", x_rot, (torch.float32,))
     samples, inp = x_rot.shape
     if factor is None:
@@ -404,6 +432,8 @@ def gptq_factor(x_rot, damp: float = 0.01, factor=None, stream=None):
 def quantize_gptq(w, grid, g: int, seed: int, factor, codes=None, scales=None, stream=None):
     """GPTQ rounding in place of Alg. 1's nearest point (same code / scale format)."""
     import torch
+    if stream is not None and _is_stream(stream):
+        return _call_on(stream, quantize_gptq, w, grid, g, seed, factor, codes, scales)
     _need_cuda("w", w, (torch.float32, torch.bfloat16))
     _need_cuda("grid", grid, (torch.float32,))
     _need_cuda("factor", factor, (torch.float64,))
@@ -429,6 +459,8 @@ def quantize_gptq(w, grid, g: int, seed: int, factor, codes=None, scales=None, s
 def rht_activations(x, g: int, seed: int, out=None, stream=None):
     """x_rot = H (sigma * x_block) / sqrt(g) per block; x: [batch, in] float32 or bfloat16."""
     _need_torch()
+    if stream is not None and _is_stream(stream):
+        return _call_on(stream, rht_activations, x, g, seed, out)
     _need_cuda("x", x, _FLOATS)
     batch, inp = x.shape
     if out is None:
@@ -446,6 +478,8 @@ def qmatmul(x_rot, codes, scales, grid, g: int, out_features: int, y=None, works
             stream=None):
     """y = rotated-space LUT product; x_rot: [batch, in] float32. Returns y [batch, out] float32."""
     _need_torch()
+    if stream is not None and _is_stream(stream):
+        return _call_on(stream, qmatmul, x_rot, codes, scales, grid, g, out_features, y, workspace)
     _need_cuda("x_rot", x_rot, _F32)
     _need_cuda("codes", codes, _U8)
     _need_cuda("scales", scales, _F16)
@@ -466,6 +500,9 @@ def qmatmul_fused(x, codes, scales, grid, g: int, seed: int, out_features: int, 
                   workspace=None, stream=None):
     """y = x W_hat^T from raw activations x: [batch, in] float32 or bfloat16."""
     _need_torch()
+    if stream is not None and _is_stream(stream):
+        return _call_on(stream, qmatmul_fused, x, codes, scales, grid, g, seed, out_features, y,
+                        workspace)
     _need_cuda("x", x, _FLOATS)
     _need_cuda("codes", codes, _U8)
     _need_cuda("scales", scales, _F16)
@@ -488,6 +525,9 @@ def qmatmul_fused_noalloc(x, codes, scales, grid, g: int, seed: int, out_feature
     """qmatmul_fused with the library's fixed scratch as the workspace (no
     device allocation by the library; calls on one device must not overlap)."""
     _need_torch()
+    if stream is not None and _is_stream(stream):
+        return _call_on(stream, qmatmul_fused_noalloc, x, codes, scales, grid, g, seed,
+                        out_features, y)
     _need_cuda("x", x, _FLOATS)
     _need_cuda("codes", codes, _U8)
     _need_cuda("scales", scales, _F16)
@@ -512,6 +552,8 @@ def qmatmul_fused_multi(x, layers, grid, g: int, ys=None, workspace=None, stream
     """Outputs of up to 4 layers that read the same raw activations x:
     layers = [(codes, scales, seed, out_features), ...]; returns [y_l]."""
     _need_torch()
+    if stream is not None and _is_stream(stream):
+        return _call_on(stream, qmatmul_fused_multi, x, layers, grid, g, ys, workspace)
     _need_cuda("x", x, _FLOATS)
     _need_cuda("grid", grid, _F32)
     batch, inp = x.shape
@@ -572,19 +614,9 @@ def _need_matrix(name, t, dtypes):
 
 
 def _mx_call_on(stream, call, first, *args):
-    """call(first, *args) with `stream` current, so that what it allocates is that stream's
-    memory: a block from the current stream's may still be in use by work queued there.
-    New results are for the current stream as well: their memory is not handed out again
-    before the work that it holds when they are released."""
     if isinstance(first, _torch.Tensor) and first.get_device() != stream.device.index:
         raise ValueError(f"tensors on {first.device}, stream on {stream.device}")
-    here = _torch.cuda.current_stream(stream.device)
-    with _torch.cuda.stream(stream):
-        results = call(first, *args)
-    for t in results if isinstance(results, tuple) else (results,):
-        if isinstance(t, _torch.Tensor) and not any(t is a for a in args):
-            t.record_stream(here)
-    return results
+    return _call_on(stream, call, first, *args)
 
 
 def _mx_stream(first, *tensors):
