@@ -22,7 +22,9 @@ inline int64_t mx_blocks(int64_t in) { return (in + kMxBlock - 1) / kMxBlock; }
 struct MxSigns {
   uint32_t w[128];
 };
-// (mx_quant.hip; computed once per seed and group size, kept per thread)
+// (mx_quant.hip; each thread keeps those of the last four pairs of seed and group size. To
+// make them takes a call's host time: one row of 4096 -> 4096 takes 6.6 us with up to four
+// seeds in turn and 10.8 with 64 for g = 1024, 11.1 and 28.9 for g = 4096)
 void mx_signs(uint64_t seed, int g, MxSigns* s);
 
 // Activations in the product's order, so that what a wave loads of a stage (128

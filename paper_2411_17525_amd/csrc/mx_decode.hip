@@ -2,8 +2,8 @@
 //
 // A block takes tiles of 16 outputs, one after another; its waves share K in
 // chunks of 512 (256 bytes of a weight row). A wave's chunk of a tile, 4 KiB, goes
-// from memory into the wave's own LDS slots, one chunk ahead and with whole lines
-// of each row, and from there into the 16x16x128 scaled matrix instruction, whose
+// from memory into the wave's own LDS slots, requested one chunk ahead and with whole
+// lines of each row, and from there into the 16x16x128 scaled matrix instruction, whose
 // other operand is up to 16 activation rows; 32 with two of them. The waves' sums
 // of a tile meet in LDS and are added in the waves' order.
 //
@@ -11,10 +11,13 @@
 // convert little (FUSED), each block rotates and quantizes them itself while its
 // first weights are on their way, into LDS: one launch instead of two.
 //
-// What bounds it is the way from memory to LDS, and with few chunks per wave the
-// latency of a chunk (2.4 us): 4 x 4096 -> 28672 takes 13.7 us (62 MB, 4.5 TB/s), 16 x
-// 14336 -> 4096 15 us behind the conversion (31 MB, 2.1 TB/s), one row of 4096 -> 4096
-// 7.3 us, of which a launch and the conversion are half. 3 slots and 14 waves gained
+// What bounds it is the way from memory to LDS where a wave has many chunks (4 x 4096 ->
+// 28672: 14.1 us among others, 62 MB, 4.4 TB/s), and where it has few its own waiting, 2.4
+// us per chunk: a request is conditional (none behind the last tile, scale bytes one by
+// one in a row's last chunk), so that the compiler cannot count the loads in flight and
+// every second step of the loop waits for all of them, the chunk just requested included
+// (16 x 14336 -> 4096: 16 us behind the conversion, 31 MB, 2 TB/s). One row of 4096 -> 4096
+// takes 7.3 us, of which a launch and the conversion are half. 3 slots and 14 waves gained
 // nothing, two blocks per compute unit with two tiles of rows lost.
 
 #include <algorithm>

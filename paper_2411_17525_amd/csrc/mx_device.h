@@ -19,7 +19,7 @@ namespace higgs {
 // lane holds half a block: its largest, codes and scale take one step across lanes.
 // (With the values in runs first, 4 + 4 bits in registers, the last two by permlane
 // swaps and the way back to runs through LDS, a segment's quantization took 650
-// instructions, not 350.)
+// instructions, not 343.)
 template <typename T>
 constexpr int kMxWaveLds = 576 * 2 * int(sizeof(T)) / 4;  // dwords per wave
 

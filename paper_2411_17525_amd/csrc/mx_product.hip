@@ -11,9 +11,10 @@
 // 4 (l / 32). The activations are the rows, the weights the columns.
 //
 // What bounds it: matrix instructions at the clock that they leave (47% of the cycles at
-// 1.75 GHz for 2048 x 4096 -> 28672 with E2M3, 148 us in two launches, 3.2 PFLOP/s), the
-// starts and outputs of tiles, which all compute units reach together, and for few tiles
-// the latency of a stage's loads.
+// 1.75 GHz for 2048 x 4096 -> 28672 with E2M3, 150 us in two launches behind a fill of the
+// caches, 3.2 PFLOP/s; the instruction alone, fed from LDS, reaches 5.7), the starts and
+// outputs of tiles, which all compute units reach together, and for few tiles the latency
+// of a stage's loads.
 
 #include <algorithm>
 
@@ -590,8 +591,10 @@ Plan plan_of(int64_t batch, int64_t out, int64_t in, int fmt, int g) {
     return p;
   }
   // Tiles that fill whole rounds of a shape as one product, the columns left over as
-  // another of smaller blocks instead of a round that leaves units idle (2048 x 4096 ->
-  // 28672: 3.5 rounds of 256 x 256; three, and one of 128 x 256, took 154 us, not 162).
+  // another of smaller blocks instead of a round that leaves units idle (in two and in one,
+  // fp32 outputs: 2048 x 4096 -> 18432 122.9 us and 127.7, 1024 x 4096 -> 35840 120.8 and
+  // 126.8, but 2048 x 1024 -> 9001 38.4 and 31.2; 2048 x 4096 -> 28672 to bf16 159.4 and
+  // 159.7).
   for (const Shape& s : kShapes) {
     const int64_t mt = (batch + s.bm - 1) / s.bm, nt = (out + s.bn - 1) / s.bn;
     const int64_t rounds = mt * nt / (kCus * s.percu);
@@ -623,8 +626,8 @@ template <int FMT, typename OutT>
 hipError_t launch_shape(int shape, Args a, hipStream_t stream) {
   a.mtiles = int((a.batch + kShapes[shape].bm - 1) / kShapes[shape].bm);
   a.ntiles = int((a.out + kShapes[shape].bn - 1) / kShapes[shape].bn);
-  // bands of equal height near four (2048 x 4096 -> 28672 takes 167 us with four row tiles,
-  // 171 with two, 176 with eight), up to six in one
+  // bands of equal height near four (2048 x 4096 -> 28672, conversion included, takes 159.4
+  // us with four row tiles, 162.0 with two, 161.3 with eight), up to six in one
   const int bands = std::max(1, (a.mtiles + 1) / 4);
   a.band = (a.mtiles + bands - 1) / bands;
   // (4-bit activations leave room for five stages of two blocks of 64 x 128: 19.0 us for 200

@@ -11,11 +11,13 @@
 //
 // With a rotation, a wavefront takes segments of 1024 values (of g for g =
 // 2048 and 4096). Rows are whole groups there, so the matrix is one run of groups.
-// What bounds these kernels is the issue of vector instructions: of the 337 that a
-// segment's quantization takes (160 of them the butterflies, in fp64 at the rate of
-// fp32), 71% of the cycles issue one; LDS is busy in 41%. 14336 x 4096 bf16 to E2M1 with
-// g = 1024: 45 to 49 us (3.2 TB/s); its layer error 46 (3.2 TB/s), the way back 35 (4.2
-// TB/s, near a copy's rate).
+// What bounds these kernels is the issue of vector instructions: a segment's quantization
+// takes 343 (160 of them the butterflies, in fp64 at the rate of fp32) and 74% of the
+// cycles issue one; LDS is busy in 41%. 14336 x 4096 bf16 to E2M1 with g = 1024, kernels
+// in a row on changing inputs: 45 to 49 us (3.0 to 3.3 TB/s), with g = 2048 50 and g = 4096
+// 62 (12% more instructions per value, and no loads ahead; two waves per SIMD for 4096);
+// its layer error 46 (3.2 TB/s), the way back 35 (4.2 TB/s, near a copy's rate). One
+// kernel by itself behind a fill of the caches takes 5 to 10 us more.
 
 #include <algorithm>
 #include <cmath>
