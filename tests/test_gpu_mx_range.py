@@ -84,7 +84,7 @@ def test_all_scale_bytes(H, g, fmt, dtype, lo, hi):
     """Any codes with scale bytes of lo .. hi - 1: the smallest, the largest, all."""
     announce(f"bytes {lo}..{hi} g={g} {fmt} {dtype}")
     rng = np.random.default_rng(g + lo + hi)
-    rows, inp = 3, 3 * g
+    rows, inp = 3, 5 * g
     packed = rng.integers(0, 256, (rows, M.row_bytes(inp, fmt)), dtype=np.uint8)
     scales = rng.integers(lo, hi, (rows, M.blocks(inp)), dtype=np.uint8)
     got = back(H, packed, scales, inp, fmt, g, 5, dtype)
